@@ -78,6 +78,16 @@ typedef enum specext_dtype {
  * that finishes last.  Results are unchanged; for testing that hand-over. */
 #define SPECEXT_FLAG_SHORT_WAIT 8u
 
+/* desc->flags, one of the three at most: the prefix is an 8-bit cache (e4m3 keys and values) with one scale for every
+ * 32, 64 or 128 tokens of a KV head; each flag's value is its number of tokens.  Such a descriptor belongs to
+ * specext_verify_attn_quant; specext_workspace_bytes, specext_num_splits and the chunk-score functions take it too, the
+ * other attention functions refuse it (SPECEXT_ERR_INVALID_ARG).  dtype has to be SPECEXT_BF16 (queries and tree),
+ * chunk_size a multiple of 32 when want_scores is set, kp_stride_* multiples of 16, and SPECEXT_FLAG_VALU_PREFIX unset
+ * (SPECEXT_ERR_UNSUPPORTED otherwise); SPECEXT_FLAG_FUSED_MERGE has no effect. */
+#define SPECEXT_FLAG_QUANT_BLOCK_32 32u
+#define SPECEXT_FLAG_QUANT_BLOCK_64 64u
+#define SPECEXT_FLAG_QUANT_BLOCK_128 128u
+
 #define SPECEXT_MAX_TREE 128           /* largest supported n_tree */
 #define SPECEXT_MAX_SPLITS 256         /* largest supported num_splits */
 #define SPECEXT_WORKSPACE_HEADER_BYTES 82176   /* head of every workspace, see specext_workspace_init */
@@ -426,6 +436,97 @@ int specext_chunk_scores_materialized(const specext_desc* desc, const void* work
  * specext_status on an invalid descriptor.
  */
 int specext_num_splits(const specext_desc* desc);
+
+/*
+ * The target's KV cache in 8 bits: half the bytes to stream per verification, twice the tokens in the same memory.
+ *
+ *   k_cache, v_cache  [n_layers, n_kv_heads, cache_capacity, head_dim] e4m3 values (OCP: largest 448, no infinities),
+ *                     one byte each
+ *   k_scale, v_scale  fp32 [n_layers, n_kv_heads, ceil(cache_capacity / scale_block)]: the value of an element of token
+ *                     j is its e4m3 value times scale[j / scale_block].  scale_block is 32, 64 or 128 tokens
+ *
+ * What specext_quant_kv_write and specext_commit_tree_quant write: scale = the smallest power of two that brings the
+ * largest finite magnitude of the block's new rows to at most 448, and not below 2^-100; where the block holds rows in
+ * front of the new ones, at least the scale that it has.  Codes are x / scale to the nearest, ties to even; infinities
+ * become +-448, NaN stays NaN.  A scale that grows moves the older rows of its block under the new one: exact for powers
+ * of two but for magnitudes below 2^-15 of the largest, which round to steps of 2^-18 of it.  Rows behind the new
+ * ones stay as they are and hold nothing until they are written (a write into a block takes the block's scale for that
+ * of its older rows only).  The readers take any positive normal scale; a prefix for specext_verify_attn_quant needs
+ * magnitudes of V within 2^-100 ... 2^100.
+ *
+ * head_dim 64 or 128; dtype is that of the caller's rows, SPECEXT_BF16 or SPECEXT_F32.  Strides are in elements
+ * (cache_stride_*: bytes; scale_stride_*: floats), 0 = contiguous in the shapes given; rows of head_dim elements are
+ * contiguous, strides in bytes multiples of 16, cache and row pointers 16-byte aligned.
+ */
+
+/*
+ * n_tokens rows enter the cache at token `start`: k_src, v_src [n_layers, n_kv_heads, n_tokens, head_dim] of dtype.
+ * start + n_tokens <= cache_capacity; n_tokens = 0 does nothing.
+ */
+int specext_quant_kv_write(const void* k_src, const void* v_src, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                           int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t n_tokens, int32_t start,
+                           int32_t cache_capacity, int32_t scale_block, int32_t dtype, int64_t src_stride_layer, int64_t src_stride_h,
+                           int64_t src_stride_t, int64_t cache_stride_layer, int64_t cache_stride_h, int64_t cache_stride_l,
+                           int64_t scale_stride_layer, int64_t scale_stride_h, void* stream);
+
+/*
+ * Rows start ... start + n_tokens - 1 of the cache as bf16 or fp32 values, k_dst, v_dst [n_layers, n_kv_heads, n_tokens,
+ * head_dim] of dtype: value = code x scale, rounded to dtype (exact in bf16 for scales that are powers of two).  For
+ * specext_prefill_attn of a later piece of a prompt, and whatever else wants the cache's rows.
+ */
+int specext_quant_kv_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, void* k_dst, void* v_dst,
+                          int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t n_tokens, int32_t start, int32_t cache_capacity,
+                          int32_t scale_block, int32_t dtype, int64_t dst_stride_layer, int64_t dst_stride_h, int64_t dst_stride_t,
+                          int64_t cache_stride_layer, int64_t cache_stride_h, int64_t cache_stride_l, int64_t scale_stride_layer,
+                          int64_t scale_stride_h, void* stream);
+
+/*
+ * specext_commit_tree_kv into an 8-bit cache: cache[y, g, prefix_len + i, :] = tree[y, g, path[i], :] for i < n_accept.
+ * path holds min(max_accept, n_tree) entries; the count is clamped to that.  An entry that is no node leaves its
+ * cache row as it is.  n_tree and max_accept <= 128, prefix_len + max_accept <= cache_capacity.
+ */
+int specext_commit_tree_quant(const void* k_tree, const void* v_tree, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                              const int32_t* path, const int32_t* n_accept, int32_t max_accept, int32_t n_tree, int32_t n_layers,
+                              int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len, int32_t cache_capacity, int32_t scale_block,
+                              int32_t dtype, int64_t tree_stride_layer, int64_t tree_stride_h, int64_t tree_stride_t,
+                              int64_t cache_stride_layer, int64_t cache_stride_h, int64_t cache_stride_l, int64_t scale_stride_layer,
+                              int64_t scale_stride_h, void* stream);
+
+/*
+ * specext_verify_attn over a prefix in 8 bits: desc with one of SPECEXT_FLAG_QUANT_BLOCK_*, k_prefix / v_prefix e4m3
+ * [Hkv, L, d] (kp_stride_* in bytes), k_scale / v_scale fp32 [Hkv, ceil(L / block)] with scale_stride_h floats from head
+ * to head (0: ceil(L / block)).  Queries, tree and everything else as there; n_tree = 1 is the decoding of one token.
+ * Logits are exact products of the e4m3 keys and the bf16 queries summed in fp32 (query elements below 2^-22 of their
+ * row's largest lose bits); probabilities enter the matrix cores as fp16, split partials cross memory as fp32, or as
+ * fp16 after a per-row power-of-two rescale with head_dim 128 and more than 128 rows per KV head.
+ * specext_chunk_scores and its kin read the same workspace with the same desc.
+ */
+int specext_verify_attn_quant(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix, const float* k_scale,
+                              const float* v_scale, const void* k_tree, const void* v_tree, const int32_t* parent, void* out, float* lse,
+                              void* workspace, size_t workspace_bytes, int64_t scale_stride_h, void* stream);
+
+/*
+ * What a verification step reads from the target's logits, and a drafting step from the draft model's: the most probable
+ * tokens (top_id with k = 1 is target_token / first_target of specext_accept_greedy), and the log probabilities of given
+ * tokens (of the drafted children of a node, of a prompt's next tokens).
+ *
+ *   logits        [n_rows, vocab] of dtype (SPECEXT_F32 or SPECEXT_BF16), element-aligned; row_stride elements from row to
+ *                 row (0 = vocab).  x = logit_scale * logits (0 = 1; 1 / temperature)
+ *   tokens        int32 [n_rows, n_given] or NULL (n_given = 0); logprob fp32 [n_rows, n_given] = x[token] - lse.  A token
+ *                 outside [0, vocab) gets minus infinity
+ *   top_id        int32 [n_rows, k], the k largest logits in descending order, the lower index first among equal ones;
+ *                 top_logprob fp32 [n_rows, k] or NULL.  k <= 64, k <= vocab
+ *   lse, entropy  fp32 [n_rows] or NULL: natural log of sum exp(x), and -sum p ln p
+ *   workspace     at least specext_token_logprobs_bytes(n_rows, vocab, k) bytes, 256-byte aligned
+ *
+ * Minus infinity bans a token.  A row of nothing else has lse and log probabilities of minus infinity, entropy 0 and the
+ * lowest indices.  A row that holds NaN or plus infinity has NaN for lse, entropy and log probabilities; NaN ranks
+ * highest.  vocab <= 2^20, n_rows <= 2^24; n_rows = 0 does nothing.  Results are bit-reproducible.
+ */
+size_t specext_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t k);
+int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride, float logit_scale,
+                           const int32_t* tokens, int32_t n_given, float* logprob, int32_t k, int32_t* top_id, float* top_logprob,
+                           float* lse, float* entropy, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aids, not part of the method: what the GPU at hand sustains in a pure

@@ -34,6 +34,10 @@ SPECEXT_FLAG_VALU_PREFIX = 1
 SPECEXT_FLAG_PREFIX_ONLY = 2
 SPECEXT_FLAG_FUSED_MERGE = 4
 SPECEXT_FLAG_SHORT_WAIT = 8
+# an 8-bit prefix with a scale for so many tokens
+SPECEXT_FLAG_QUANT_BLOCK_32 = 32
+SPECEXT_FLAG_QUANT_BLOCK_64 = 64
+SPECEXT_FLAG_QUANT_BLOCK_128 = 128
 WORKSPACE_HEADER_BYTES = 82176
 
 STATUS_NAMES = {0: "SPECEXT_OK", -1: "SPECEXT_ERR_INVALID_ARG", -2: "SPECEXT_ERR_UNSUPPORTED",
@@ -44,7 +48,9 @@ EXPORTED = ("specext_strerror", "specext_workspace_bytes", "specext_num_splits",
             "specext_commit_tree_kv", "specext_chunk_scores_accepted", "specext_materialized_bytes",
             "specext_materialized_ld", "specext_attn_materialized", "specext_chunk_scores_materialized",
             "specext_prefill_attn", "specext_verify_attn_static", "specext_workspace_init",
-            "specext_calib_stream_read", "specext_calib_mfma", "specext_calib_issue_mix", "specext_chunk_scores_select")
+            "specext_calib_stream_read", "specext_calib_mfma", "specext_calib_issue_mix", "specext_chunk_scores_select",
+            "specext_quant_kv_write", "specext_quant_kv_read", "specext_commit_tree_quant", "specext_verify_attn_quant",
+            "specext_token_logprobs_bytes", "specext_token_logprobs")
 
 
 class SpecextError(RuntimeError):
@@ -134,6 +140,18 @@ def load_library() -> ctypes.CDLL:
     lib.specext_calib_mfma.argtypes = [i32, i32, i32, vp, vp]
     lib.specext_calib_issue_mix.restype = ctypes.c_int
     lib.specext_calib_issue_mix.argtypes = [i32, i32, i32, i32, vp, vp]
+    lib.specext_verify_attn_quant.restype = ctypes.c_int
+    lib.specext_verify_attn_quant.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, i64, vp]
+    lib.specext_quant_kv_write.restype = ctypes.c_int
+    lib.specext_quant_kv_write.argtypes = [vp] * 6 + [i32] * 8 + [i64] * 8 + [vp]
+    lib.specext_quant_kv_read.restype = ctypes.c_int
+    lib.specext_quant_kv_read.argtypes = [vp] * 6 + [i32] * 8 + [i64] * 8 + [vp]
+    lib.specext_commit_tree_quant.restype = ctypes.c_int
+    lib.specext_commit_tree_quant.argtypes = [vp] * 8 + [i32] * 9 + [i64] * 8 + [vp]
+    lib.specext_token_logprobs_bytes.restype = sz
+    lib.specext_token_logprobs_bytes.argtypes = [i32, i32, i32]
+    lib.specext_token_logprobs.restype = ctypes.c_int
+    lib.specext_token_logprobs.argtypes = [vp, i32, i32, i32, i64, ctypes.c_float, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     _take_over()            # built since this module was imported
     if _marshal is not None:
@@ -397,6 +415,79 @@ def chunk_scores_select(desc, workspace, score_row: int, k: int, idx_out, n_out,
                                                     _ptr(idx_out), _ptr(n_out), _stream(stream))
     if check:
         _check(rc, "specext_chunk_scores_select")
+    return rc
+
+
+def verify_attn_quant(desc, q, k_prefix, v_prefix, k_scale, v_scale, k_tree, v_tree, parent, out, lse, workspace,
+                      workspace_nbytes: Optional[int] = None, scale_stride_h: int = 0, stream=None, check: bool = True) -> int:
+    if workspace_nbytes is None:
+        workspace_nbytes = workspace.numel() * workspace.element_size()
+    rc = load_library().specext_verify_attn_quant(ctypes.byref(desc), _ptr(q), _ptr(k_prefix), _ptr(v_prefix), _ptr(k_scale),
+                                                  _ptr(v_scale), _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(out), _ptr(lse),
+                                                  _ptr(workspace), workspace_nbytes, int(scale_stride_h), _stream(stream))
+    if check:
+        _check(rc, "specext_verify_attn_quant")
+    return rc
+
+
+def quant_kv_write(k_src, v_src, k_cache, v_cache, k_scale, v_scale, n_layers: int, n_kv_heads: int, head_dim: int, n_tokens: int,
+                   start: int, cache_capacity: int, scale_block: int, dtype: int = SPECEXT_BF16, src_stride_layer: int = 0,
+                   src_stride_h: int = 0, src_stride_t: int = 0, cache_stride_layer: int = 0, cache_stride_h: int = 0,
+                   cache_stride_l: int = 0, scale_stride_layer: int = 0, scale_stride_h: int = 0, stream=None, check: bool = True) -> int:
+    rc = load_library().specext_quant_kv_write(_ptr(k_src), _ptr(v_src), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                               int(n_layers), int(n_kv_heads), int(head_dim), int(n_tokens), int(start),
+                                               int(cache_capacity), int(scale_block), int(dtype), int(src_stride_layer),
+                                               int(src_stride_h), int(src_stride_t), int(cache_stride_layer), int(cache_stride_h),
+                                               int(cache_stride_l), int(scale_stride_layer), int(scale_stride_h), _stream(stream))
+    if check:
+        _check(rc, "specext_quant_kv_write")
+    return rc
+
+
+def quant_kv_read(k_cache, v_cache, k_scale, v_scale, k_dst, v_dst, n_layers: int, n_kv_heads: int, head_dim: int, n_tokens: int,
+                  start: int, cache_capacity: int, scale_block: int, dtype: int = SPECEXT_BF16, dst_stride_layer: int = 0,
+                  dst_stride_h: int = 0, dst_stride_t: int = 0, cache_stride_layer: int = 0, cache_stride_h: int = 0,
+                  cache_stride_l: int = 0, scale_stride_layer: int = 0, scale_stride_h: int = 0, stream=None, check: bool = True) -> int:
+    rc = load_library().specext_quant_kv_read(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(k_dst), _ptr(v_dst),
+                                              int(n_layers), int(n_kv_heads), int(head_dim), int(n_tokens), int(start),
+                                              int(cache_capacity), int(scale_block), int(dtype), int(dst_stride_layer),
+                                              int(dst_stride_h), int(dst_stride_t), int(cache_stride_layer), int(cache_stride_h),
+                                              int(cache_stride_l), int(scale_stride_layer), int(scale_stride_h), _stream(stream))
+    if check:
+        _check(rc, "specext_quant_kv_read")
+    return rc
+
+
+def commit_tree_quant(k_tree, v_tree, k_cache, v_cache, k_scale, v_scale, path, n_accept, max_accept: int, n_tree: int, n_layers: int,
+                      n_kv_heads: int, head_dim: int, prefix_len: int, cache_capacity: int, scale_block: int, dtype: int = SPECEXT_BF16,
+                      tree_stride_layer: int = 0, tree_stride_h: int = 0, tree_stride_t: int = 0, cache_stride_layer: int = 0,
+                      cache_stride_h: int = 0, cache_stride_l: int = 0, scale_stride_layer: int = 0, scale_stride_h: int = 0,
+                      stream=None, check: bool = True) -> int:
+    rc = load_library().specext_commit_tree_quant(_ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                                  _ptr(path), _ptr(n_accept), int(max_accept), int(n_tree), int(n_layers),
+                                                  int(n_kv_heads), int(head_dim), int(prefix_len), int(cache_capacity), int(scale_block),
+                                                  int(dtype), int(tree_stride_layer), int(tree_stride_h), int(tree_stride_t),
+                                                  int(cache_stride_layer), int(cache_stride_h), int(cache_stride_l),
+                                                  int(scale_stride_layer), int(scale_stride_h), _stream(stream))
+    if check:
+        _check(rc, "specext_commit_tree_quant")
+    return rc
+
+
+def token_logprobs_bytes(n_rows: int, vocab: int, k: int) -> int:
+    return int(load_library().specext_token_logprobs_bytes(int(n_rows), int(vocab), int(k)))
+
+
+def token_logprobs(logits, n_rows: int, vocab: int, workspace, dtype: int = SPECEXT_BF16, row_stride: int = 0, logit_scale: float = 0.0,
+                   tokens=None, n_given: int = 0, logprob=None, k: int = 0, top_id=None, top_logprob=None, lse=None, entropy=None,
+                   workspace_nbytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    if workspace_nbytes is None:
+        workspace_nbytes = workspace.numel() * workspace.element_size()
+    rc = load_library().specext_token_logprobs(_ptr(logits), int(dtype), int(n_rows), int(vocab), int(row_stride), float(logit_scale),
+                                               _ptr(tokens), int(n_given), _ptr(logprob), int(k), _ptr(top_id), _ptr(top_logprob),
+                                               _ptr(lse), _ptr(entropy), _ptr(workspace), workspace_nbytes, _stream(stream))
+    if check:
+        _check(rc, "specext_token_logprobs")
     return rc
 
 

@@ -66,8 +66,10 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   // bounds that keep the 32-bit length arithmetic below exact (rounding a length up to a chunk or a split unit)
   if (d->prefix_len > (1 << 30) || (d->want_scores && d->chunk_size > (1 << 24))) return SPECEXT_ERR_UNSUPPORTED;
   if (!(d->softmax_scale >= 0.f) || std::isinf(d->softmax_scale)) return SPECEXT_ERR_INVALID_ARG;
+  const uint32_t quant_block = d->flags & kQuantFlags;
   if (d->reserved != 0 || (d->flags & ~(SPECEXT_FLAG_VALU_PREFIX | SPECEXT_FLAG_PREFIX_ONLY | SPECEXT_FLAG_FUSED_MERGE |
-                                       SPECEXT_FLAG_SHORT_WAIT)) != 0) return SPECEXT_ERR_INVALID_ARG;
+                                       SPECEXT_FLAG_SHORT_WAIT | kQuantFlags)) != 0) return SPECEXT_ERR_INVALID_ARG;
+  if ((quant_block & (quant_block - 1)) != 0) return SPECEXT_ERR_INVALID_ARG;
   if (d->dtype != SPECEXT_F32 && d->dtype != SPECEXT_BF16) return SPECEXT_ERR_UNSUPPORTED;
   if (d->out_dtype != SPECEXT_F32 && d->out_dtype != d->dtype) return SPECEXT_ERR_UNSUPPORTED;
   if (d->head_dim != 64 && d->head_dim != 128) return SPECEXT_ERR_UNSUPPORTED;
@@ -101,6 +103,10 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   for (int64_t s : strides)
     if (s < 0 || s % 8 != 0) return SPECEXT_ERR_UNSUPPORTED;
   if (p->q_sh < p->d || p->kp_sl < p->d || p->kt_st < p->d || p->o_sh < p->d) return SPECEXT_ERR_INVALID_ARG;
+  // a prefix in 8 bits: one kernel, rows of 16-byte pieces
+  if (quant_block && (d->dtype != SPECEXT_BF16 || (p->want_scores && p->B % 32 != 0) || (d->flags & SPECEXT_FLAG_VALU_PREFIX) ||
+                      p->kp_sh % 16 != 0 || p->kp_sl % 16 != 0))
+    return SPECEXT_ERR_UNSUPPORTED;
 
   // Which prefix kernel runs.  The matrix-core kernels take bf16, d = 128, at least one
   // full 32-key tile and, when scores are wanted, chunk sizes that are whole tiles.
@@ -123,7 +129,11 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   // Everything else of bf16 and all of fp32: the matrix-core kernel with fp32 probabilities, unless the chunks are no
   // whole numbers of its four-key score blocks or a key stride leaves its 32-bit offsets within a tile.
   const bool f32_ok = (!p->want_scores || p->B % 4 == 0) && !(d->flags & SPECEXT_FLAG_VALU_PREFIX) && p->kp_sl <= (1 << 22);
-  if (mfma64_ok) {
+  if (quant_block) {
+    p->use_mfma = 4;
+    p->rows_per_group = p->M <= 32 ? 32 : p->M <= 64 ? 64 : p->M <= 128 ? 128 : 256;
+    p->part_f16 = 0;
+  } else if (mfma64_ok) {
     p->use_mfma = 2;
     p->rows_per_group = p->M > 128 ? 256 : 128;
     p->part_f16 = 0;
@@ -286,6 +296,7 @@ int resolve_materialized(const specext_desc* d, MatParams* mp, MatLayout* w) {
   const int rc = resolve(d, &mp->a);
   if (rc != SPECEXT_OK) return rc;
   const AttnParams& a = mp->a;
+  if (a.use_mfma == 4) return SPECEXT_ERR_INVALID_ARG;
   if (a.in_dtype != SPECEXT_BF16 || a.d != 128) return SPECEXT_ERR_UNSUPPORTED;
   const int64_t n = static_cast<int64_t>(a.L) + a.T;
   const int64_t ld = (n + 63) / 64 * 64;
@@ -338,10 +349,11 @@ void* static_scratch_of_current_device() {
 int verify_attn_on(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix,
                    const void* k_tree, const void* v_tree, const int32_t* parent, void* out, float* lse,
                    void* workspace, size_t workspace_bytes, int32_t* status_word, bool library_memory, bool stage_cut,
-                   void* stream) {
+                   const QuantScales* scales, LaunchPrefixQuant launch_quant, void* stream) {
   AttnParams p;
   const int rc = resolve(desc, &p, stage_cut);
   if (rc != SPECEXT_OK) return rc;
+  if ((p.use_mfma == 4) != (scales != nullptr)) return SPECEXT_ERR_INVALID_ARG;     // the prefix is in 8 bits, or it is not
   if (!q || !k_tree || !v_tree || !parent || !out || !workspace) return SPECEXT_ERR_INVALID_ARG;
   if (p.L > 0 && (!k_prefix || !v_prefix)) return SPECEXT_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_prefix) || !aligned16(v_prefix) || !aligned16(k_tree) || !aligned16(v_tree) ||
@@ -363,7 +375,8 @@ int verify_attn_on(const specext_desc* desc, const void* q, const void* k_prefix
   if (status_word) p.status = status_word;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.S > 0) {
-    const hipError_t e = p.use_mfma == 2   ? launch_prefix_mfma_rows(p, s)
+    const hipError_t e = scales            ? launch_quant(p, *scales, s)
+                         : p.use_mfma == 2 ? launch_prefix_mfma_rows(p, s)
                          : p.use_mfma == 1 ? launch_prefix_mfma(p, s)
                                            : launch_prefix_generic(p, s);
     if (e != hipSuccess) return SPECEXT_ERR_LAUNCH_FAILED;
@@ -374,6 +387,14 @@ int verify_attn_on(const specext_desc* desc, const void* q, const void* k_prefix
 }
 
 }  // namespace
+
+int verify_attn_quant_on(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix, const QuantScales& scales,
+                         const void* k_tree, const void* v_tree, const int32_t* parent, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes, LaunchPrefixQuant launch, void* stream) {
+  return verify_attn_on(desc, q, k_prefix, v_prefix, k_tree, v_tree, parent, out, lse, workspace, workspace_bytes, nullptr, false, false,
+                        &scales, launch, stream);
+}
+
 }  // namespace specext
 
 using namespace specext;
@@ -432,7 +453,7 @@ int specext_verify_attn(const specext_desc* desc, const void* q, const void* k_p
                         const void* k_tree, const void* v_tree, const int32_t* parent, void* out, float* lse,
                         void* workspace, size_t workspace_bytes, void* stream) {
   return verify_attn_on(desc, q, k_prefix, v_prefix, k_tree, v_tree, parent, out, lse, workspace, workspace_bytes,
-                        nullptr, false, false, stream);
+                        nullptr, false, false, nullptr, nullptr, stream);
 }
 
 int specext_verify_attn_static(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix,
@@ -443,6 +464,7 @@ int specext_verify_attn_static(const specext_desc* desc, const void* q, const vo
   if (rc != SPECEXT_OK) return rc;
   // the chunk partial sums would have to outlive the call for specext_chunk_scores, which
   // takes the caller's workspace: the layer that feeds the retrieval uses specext_verify_attn
+  if (p.use_mfma == 4) return SPECEXT_ERR_INVALID_ARG;
   if (p.want_scores) return SPECEXT_ERR_UNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(status_out) & 3u) return SPECEXT_ERR_UNSUPPORTED;
   bool stage_cut = false;
@@ -454,7 +476,7 @@ int specext_verify_attn_static(const specext_desc* desc, const void* q, const vo
   void* ws = static_scratch_of_current_device();
   if (!ws) return SPECEXT_ERR_LAUNCH_FAILED;
   return verify_attn_on(desc, q, k_prefix, v_prefix, k_tree, v_tree, parent, out, lse, ws, kStaticScratchBytes,
-                        status_out, true, stage_cut, stream);
+                        status_out, true, stage_cut, nullptr, nullptr, stream);
 }
 
 int specext_chunk_scores(const specext_desc* desc, const void* workspace, size_t workspace_bytes,

@@ -55,7 +55,7 @@ struct AttnParams {
   int32_t Hq, Hkv, G, d, L, T, M;
   int32_t B, C, S, keys_per_split, want_scores;
   int32_t score_gran, n_sub;      // keys per score block (32: bf16 matrix-core kernels; 4, 8 or 16: fp32-probability kernel; else B) and their count
-  int32_t use_mfma;               // 0 vector-ALU kernel; matrix cores: 1 key-split, 2 row-split, 3 fp32-probability kernel
+  int32_t use_mfma;               // 0 vector-ALU kernel; matrix cores: 1 key-split, 2 row-split, 3 fp32-probability kernel, 4 8-bit prefix
   int32_t rows_per_group;         // query rows of one KV head that one workgroup covers
   int32_t part_f16;               // part_o [S][rows][d] holds the unnormalised O as fp16 (1: row-split kernel) or fp32 (0)
   int32_t fused_tail;             // 1: the row-split kernel also runs the tree pass and the merge (no second launch)
@@ -65,6 +65,16 @@ struct AttnParams {
   float scale_log2;
   int64_t q_st, q_sh, kp_sh, kp_sl, kt_sh, kt_st, o_st, o_sh;
 };
+
+// The scales of an 8-bit prefix: [Hkv][sh], one for every `block` keys, for K and for V.  Beside AttnParams, whose size every
+// other kernel's launch pays for.
+struct QuantScales {
+  const float* k;
+  const float* v;
+  int64_t sh;
+  int32_t block_log2;
+};
+constexpr uint32_t kQuantFlags = SPECEXT_FLAG_QUANT_BLOCK_32 | SPECEXT_FLAG_QUANT_BLOCK_64 | SPECEXT_FLAG_QUANT_BLOCK_128;
 
 // Standard attention with the probability matrix written out (the score path of
 // Sec. 3.2.1 as the paper describes it): the problem plus the two buffers it needs.
@@ -91,6 +101,12 @@ struct PrefillParams {
   int64_t q_st, q_sh, k_sh, k_sl, o_st, o_sh;
 };
 
+// specext_verify_attn over an 8-bit prefix: checks, workspace and merge of api.hip around the prefix pass that is handed in
+using LaunchPrefixQuant = hipError_t (*)(const AttnParams&, const QuantScales&, hipStream_t);
+int verify_attn_quant_on(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix, const QuantScales& scales,
+                         const void* k_tree, const void* v_tree, const int32_t* parent, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes, LaunchPrefixQuant launch, void* stream);
+
 // Launchers (each returns a hipError_t from the launch itself).
 hipError_t launch_prefill_rows(const PrefillParams& p, hipStream_t stream);
 hipError_t launch_materialized(const MatParams& mp, hipStream_t stream);
@@ -100,6 +116,7 @@ hipError_t launch_prefix_generic(const AttnParams& p, hipStream_t stream);     /
 hipError_t launch_prefix_f32(const AttnParams& p, hipStream_t stream);         // fp32-probability kernel
 hipError_t launch_prefix_mfma(const AttnParams& p, hipStream_t stream);        // key-split kernel (use_mfma == 1)
 hipError_t launch_prefix_mfma_rows(const AttnParams& p, hipStream_t stream);   // row-split kernel (use_mfma == 2)
+hipError_t launch_prefix_quant(const AttnParams& p, const QuantScales& scales, hipStream_t stream);   // 8-bit prefix (use_mfma == 4)
 hipError_t launch_tree_merge(const AttnParams& p, hipStream_t stream);
 // score_row >= 0: that row; -1: every row; row_path != nullptr: the row is read on the device,
 // row_path[*row_count - 1] (row 0 when *row_count <= 0)

@@ -1,0 +1,242 @@
+"""Hybrid Tree Attention over an 8-bit prefix against the same attention in 64 bits on the values that the cache stands for.
+
+Tolerances.  A probability is rounded to fp16 (2^-11 of it; below 2^-14 of the reference 2^-25 of the reference, and a row's sum is
+at least one), a partial output to fp16 against its row's largest element (2^-11), sums are fp32 (n additions of 2^-24): together
+under 2^-10 + n 2^-24 of the row's largest sum of p |v|.  The result is rounded to its type (2^-8 of it in bf16).  A logit is a sum
+of d + 1 fp32 roundings, 2^-24 each, of at most `spread` = scale sum |q k|: under 2^-16 of it with the exponential's own; the
+log-sum-exp and the probabilities follow the logits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import quant_util as qu
+
+pytestmark = pytest.mark.gpu
+
+
+class _Problem:
+    def __init__(self, seed, d, hq, hkv, t, n, block, gap=0, parent=None, scales=None, sharp=1.0):
+        rng = np.random.default_rng(seed)
+        self.d, self.hq, self.hkv, self.t, self.n, self.block = d, hq, hkv, t, n, block
+        self.cap = n + gap
+        bf = lambda *s: torch.from_numpy((rng.standard_normal(s) * 1.0).astype(np.float32)).bfloat16()  # noqa: E731
+        self.q, self.k_tree, self.v_tree = bf(t, hq, d) * sharp, bf(hkv, t, d), bf(hkv, t, d)
+        self.parent = qu.random_tree(t, rng) if parent is None else parent
+        nb = -(-self.cap // block)
+        self.codes, self.scale, self.value = {}, {}, {}
+        for name in "kv":
+            # e4m3 values of normal numbers; behind the prefix NaN codes and NaN scales
+            raw = torch.from_numpy(rng.standard_normal((hkv, self.cap, d)).astype(np.float32) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+            u = raw.view(torch.uint8).clone()
+            u[:, n:] = 0x7F
+            s = 2.0 ** -7 * np.exp2(rng.integers(-2, 3, (hkv, nb))).astype(np.float32) if scales is None else scales(rng, name, (hkv, nb))
+            s = torch.from_numpy(np.asarray(s, dtype=np.float32).copy())
+            self.value[name] = u[:, :n].view(torch.float8_e4m3fn).double() * s.double().repeat_interleave(block, 1)[:, :n, None]
+            s[:, -(-n // block):] = math.nan
+            self.codes[name], self.scale[name] = u, s
+
+    def reference(self, chunk=None, softmax_scale=0.0):
+        scale = softmax_scale or 1 / math.sqrt(self.d)
+        return qu.attention(self.q.double(), self.value["k"], self.value["v"], self.k_tree.double(), self.v_tree.double(), self.parent, scale, chunk)
+
+    def run(self, chunk=0, out_f32=False, num_splits=0, softmax_scale=0.0, stream=None, layout="heads", rows=None):
+        import paper_2505_20776_amd as sx
+        from paper_2505_20776_amd import harness as hx
+        dev = {name: self.codes[name].cuda() for name in "kv"}
+        strides = dict(kp_stride_h=self.cap * self.d, kp_stride_l=self.d)
+        if layout == "tokens":
+            dev = {name: x.permute(1, 0, 2).contiguous() for name, x in dev.items()}
+            strides = dict(kp_stride_h=self.d, kp_stride_l=self.hkv * self.d)
+        desc = sx.make_desc(dtype=sx.SPECEXT_BF16, out_dtype=sx.SPECEXT_F32 if out_f32 else sx.SPECEXT_BF16, n_q_heads=self.hq,
+                            n_kv_heads=self.hkv, head_dim=self.d, prefix_len=self.n, n_tree=self.t, chunk_size=chunk, want_scores=chunk > 0,
+                            num_splits=num_splits, softmax_scale=softmax_scale, flags=self.block, **strides)
+        made = {"ws": hx.guarded((sx.workspace_bytes(desc),), torch.uint8), "lse": hx.guarded((self.hq, self.t), torch.float32),
+                "out": hx.guarded((self.t, self.hq, self.d), torch.float32 if out_f32 else torch.bfloat16)}
+        ws, lse, out = (made[x][0] for x in ("ws", "lse", "out"))
+        dev = {**dev, "q": self.q.cuda(), "kt": self.k_tree.cuda(), "vt": self.v_tree.cuda(), "p": torch.from_numpy(self.parent).cuda(),
+               "ks": self.scale["k"].cuda(), "vs": self.scale["v"].cuda()}
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        call = lambda: sx.verify_attn_quant(desc, dev["q"], dev["k"], dev["v"], dev["ks"], dev["vs"], dev["kt"], dev["vt"], dev["p"], out, lse, ws,  # noqa: E731
+                                            scale_stride_h=dev["ks"].shape[1], stream=stream)
+        call()
+        scores = None
+        if chunk:
+            n_chunks = -(-self.n // chunk)
+            scores, made["scores"] = hx.guarded((self.t, n_chunks), torch.float32)
+            sx.chunk_scores(desc, ws, -1, scores, stream=stream)
+        torch.cuda.synchronize()
+        assert int(ws[:4].view(torch.int32)) == 0
+        for name, (_, base) in [(k, v) for k, v in made.items() if isinstance(v, tuple)]:
+            assert hx.guards_intact(base), name
+        self.call, self.out, self.lse, self.kept = call, out, lse, dev
+        return out.cpu().double(), lse.cpu().double(), None if scores is None else scores.cpu().double()
+
+    def check(self, chunk=0, out_f32=False, **kw):
+        out, lse, scores = self.run(chunk, out_f32, **kw)
+        want, want_lse, mag, spread, want_scores = self.reference(chunk or None, kw.get("softmax_scale", 0.0))
+        off_logit = 2.0 ** -16 * spread
+        tol = (2.0 ** -10 + (self.n + self.t) * 2.0 ** -24 + 2 * off_logit.T)[:, :, None] * mag[:, :, None] + (0 if out_f32 else 2.0 ** -8) * want.abs()
+        worst = ((out - want).abs() / tol).max()
+        assert worst <= 1, f"out is {worst:.2f} tolerances off"
+        assert ((lse - want_lse).abs() <= off_logit + 2.0 ** -18 * (1 + want_lse.abs())).all()
+        if chunk:
+            rel = (2 * off_logit.amax(dim=0) + 2.0 ** -16)[:, None]
+            assert ((scores - want_scores).abs() <= rel * want_scores.amax(dim=1, keepdim=True)).all()
+
+
+# rows per KV head: at most 32, 64, 128, and more (one group of 256 rows, two)
+ROWS = [(32, 8, 1), (32, 8, 8), (8, 8, 32), (32, 8, 9), (4, 2, 32), (32, 32, 60), (12, 1, 10), (32, 8, 32), (8, 1, 17), (32, 8, 60), (8, 2, 64),
+        (2, 1, 128), (8, 1, 128)]
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("hq,hkv,t", ROWS)
+def test_row_counts(d, hq, hkv, t):
+    p = _Problem(hq * t + d, d, hq, hkv, t, 777, 32 if t % 2 else 64, gap=40)
+    p.check(chunk=64)
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 200, 257, 1000, 5003])
+@pytest.mark.parametrize("d,hq,hkv,t,block", [(128, 8, 2, 3, 32), (128, 8, 2, 15, 64), (128, 8, 2, 60, 128), (128, 4, 1, 30, 32), (64, 6, 2, 7, 128), (64, 4, 1, 50, 32)])
+def test_lengths(d, hq, hkv, t, block, n):
+    print(f"[case] d={d} heads={hq}/{hkv} t={t} block={block} n={n}", flush=True)
+    _Problem(n + d + t, d, hq, hkv, t, n, block, gap=n % 3 * 50).check(chunk=32 if n % 2 else 96)
+
+
+@pytest.mark.parametrize("splits", [1, 2, 3, 7, 40, 256])
+@pytest.mark.parametrize("d,t", [(128, 4), (128, 16), (128, 30), (128, 60), (64, 60), (64, 5)])
+def test_requested_splits(d, t, splits):
+    _Problem(d * t + splits, d, 8, 2, t, 1237, 64).check(num_splits=splits, chunk=32)
+
+
+@pytest.mark.parametrize("d,t", [(128, 8), (128, 60), (64, 20)])
+def test_layouts_outputs_and_scales(d, t):
+    """Token-major cache; fp32 output; an explicit softmax scale; scales of any value."""
+    any_scale = lambda rng, name, shape: rng.uniform(0.003, 0.03, shape)  # noqa: E731
+    _Problem(1, d, 8, 4, t, 500, 32, gap=12, scales=any_scale).check(layout="tokens", out_f32=True)
+    _Problem(2, d, 8, 4, t, 500, 128, scales=any_scale).check(softmax_scale=0.31, chunk=32)
+
+
+@pytest.mark.parametrize("d,t", [(128, 8), (128, 20), (128, 60), (64, 20)])
+def test_values_of_any_size(d, t):
+    """Scales of V that differ by 2^40 from block to block, or are as small as the writer makes them; none of K matter but for the
+    logits."""
+    def wild(rng, name, shape):
+        return np.exp2(rng.integers(-30, 11, shape)) if name == "v" else np.full(shape, 0.01)
+    _Problem(5, d, 8, 4, t, 700, 32, scales=wild).check()
+    for e in (-80, 80):
+        p = _Problem(6, d, 8, 4, t, 300, 64, scales=lambda rng, name, shape: np.full(shape, 2.0 ** e if name == "v" else 0.01))
+        p.v_tree = (p.v_tree.double() * 2.0 ** e).bfloat16()
+        p.check(out_f32=True)
+
+    def zeros(rng, name, shape):              # blocks of zeros, as written: scale 2^-100
+        s = np.full(shape, 0.01)
+        if name == "v":
+            s[:, ::2] = 2.0 ** -100
+        return s
+    p = _Problem(7, d, 8, 4, t, 400, 32, scales=zeros)
+    for b in range(0, 13, 2):
+        p.codes["v"][:, 32 * b:32 * b + 32] = 0
+    p.value["v"] = p.codes["v"][:, :400].view(torch.float8_e4m3fn).double() * p.scale["v"].double().repeat_interleave(32, 1)[:, :400, None]
+    p.check(chunk=32)
+
+
+@pytest.mark.parametrize("t", [8, 60])
+def test_sharp_rows(t):
+    """Logits of several hundred: the running reference moves, most probabilities vanish."""
+    _Problem(8, 128, 8, 2, t, 900, 32, sharp=16.0).check(chunk=32)
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -60, 2.0 ** 60])
+def test_queries_of_any_size(factor):
+    p = _Problem(9, 128, 8, 2, 20, 300, 32)
+    p.q = (p.q.double() * factor).bfloat16()
+    p.q[3] = 0
+    p.check(softmax_scale=float(np.float32(0.1 / factor)))
+
+
+def test_no_prefix():
+    for t in (1, 60):
+        p = _Problem(10, 128, 8, 2, t, 0, 32, gap=32)
+        p.check()
+
+
+def test_malformed_parent_is_reported():
+    import paper_2505_20776_amd as sx
+    p = _Problem(11, 128, 4, 2, 4, 64, 32)
+    p.run()
+    p.kept["p"][2] = 3
+    ws = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+    desc = sx.make_desc(dtype=sx.SPECEXT_BF16, n_q_heads=4, n_kv_heads=2, head_dim=128, prefix_len=64, n_tree=4, flags=32)
+    d = p.kept
+    sx.verify_attn_quant(desc, d["q"], d["k"], d["v"], d["ks"], d["vs"], d["kt"], d["vt"], d["p"], p.out, p.lse, ws)
+    torch.cuda.synchronize()
+    assert int(ws[:4].view(torch.int32)) == 1
+
+
+@pytest.mark.parametrize("t", [1, 60])
+def test_side_stream_and_repeats(t):
+    """On another stream; and bit for bit the same again."""
+    p = _Problem(12, 128, 8, 2, t, 600, 32)
+    p.check(stream=torch.cuda.Stream())
+    first = p.out.clone()
+    for _ in range(3):
+        p.out.zero_()
+        p.call()
+        torch.cuda.synchronize()
+        assert torch.equal(first, p.out)
+
+
+def test_captured_and_replayed():
+    p = _Problem(13, 128, 8, 2, 20, 600, 32)
+    p.check()
+    eager = p.out.clone(), p.lse.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    import paper_2505_20776_amd as sx  # noqa: F401
+    with torch.cuda.graph(graph, stream=side):
+        p.call()
+    for _ in range(3):
+        p.out.zero_()
+        p.lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(p.out, eager[0]) and torch.equal(p.lse, eager[1])
+        p.call()
+        torch.cuda.synchronize()
+        assert torch.equal(p.out, eager[0])
+
+
+def test_cache_beyond_32_bits():
+    """Offsets within one head's keys that pass 2^32 bytes: a token-major cache of 2^22 tokens whose rows are 1 KB apart, attended in its
+    last 300 tokens through a small prefix, and in whole by one node."""
+    import paper_2505_20776_amd as sx
+    d, n, block = 64, (1 << 22) + 77, 128
+    stride = 1024
+    k = torch.zeros((n, stride), dtype=torch.uint8, device="cuda")
+    nb = -(-n // block)
+    ks = torch.full((1, nb), 0.01, dtype=torch.float32, device="cuda")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    # only the last keys carry weight: large keys along the query
+    q = torch.ones((1, 1, d), dtype=torch.bfloat16, device="cuda")
+    last = torch.randint(0x40, 0x50, (300, d), generator=gen, device="cuda", dtype=torch.uint8)
+    k[-300:, :d] = last
+    kt = torch.zeros((1, 1, d), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty((1, 1, d), dtype=torch.float32, device="cuda"), torch.empty((1, 1), dtype=torch.float32, device="cuda")
+    desc = sx.make_desc(dtype=sx.SPECEXT_BF16, out_dtype=sx.SPECEXT_F32, n_q_heads=1, n_kv_heads=1, head_dim=d, prefix_len=n, n_tree=1,
+                        kp_stride_h=n * stride, kp_stride_l=stride, flags=block, softmax_scale=10.0)
+    ws = torch.empty(sx.workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    sx.verify_attn_quant(desc, q, k, k, ks, ks, kt, kt, torch.tensor([-1], dtype=torch.int32, device="cuda"), out, lse, ws)
+    torch.cuda.synchronize()
+    x = last.cpu().view(torch.float8_e4m3fn).double() * float(np.float32(0.01))
+    s = x.sum(dim=1) * 10.0
+    zeros = n - 300 + 1
+    total = torch.logsumexp(torch.cat([s, torch.tensor([math.log(zeros)], dtype=torch.float64)]), 0)
+    want = torch.exp(s - total) @ x
+    assert abs(float(lse) - float(total)) <= 2.0 ** -16 * float(s.max())
+    assert ((out.cpu().double() - want).abs() <= 2.0 ** -9 * want.abs().max()).all()
