@@ -148,10 +148,14 @@ size_t stats_bytes(int32_t n_rows, int slices) { return align_up(static_cast<siz
 
 size_t specext_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t k) {
   if (!logprob_shape_ok(n_rows, vocab, k)) return 0;
-  const LogprobCut cut = logprob_cut(vocab);
-  if (cut.slices == 1) return kAlign;
-  const size_t need = stats_bytes(n_rows, cut.slices) + align_up(static_cast<size_t>(n_rows) * cut.slices * k * sizeof(unsigned long long));
-  return need > kAlign ? need : kAlign;
+  size_t most = kAlign;
+  for (const bool bf16 : {false, true}) {
+    const LogprobCut cut = logprob_cut(n_rows, vocab, bf16);
+    if (cut.slices == 1) continue;
+    const size_t need = stats_bytes(n_rows, cut.slices) + align_up(static_cast<size_t>(n_rows) * cut.slices * k * sizeof(unsigned long long));
+    if (need > most) most = need;
+  }
+  return most;
 }
 
 int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride, float logit_scale,
@@ -167,7 +171,7 @@ int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, in
       !aligned(top_logprob, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(workspace, kAlign))
     return SPECEXT_ERR_UNSUPPORTED;
   if (workspace_bytes < specext_token_logprobs_bytes(n_rows, vocab, k)) return SPECEXT_ERR_WORKSPACE_TOO_SMALL;
-  const LogprobCut cut = logprob_cut(vocab);
+  const LogprobCut cut = logprob_cut(n_rows, vocab, dtype == SPECEXT_BF16);
   if (static_cast<int64_t>(n_rows) * cut.slices > (int64_t{1} << 30)) return SPECEXT_ERR_UNSUPPORTED;
   LogprobArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -176,7 +180,7 @@ int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, in
   a.keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + stats_bytes(n_rows, cut.slices));
   a.row_stride = stride, a.bf16 = dtype == SPECEXT_BF16, a.n_rows = n_rows, a.vocab = vocab, a.n_given = n_given, a.k = k;
   a.slices = cut.slices, a.logit_scale = logit_scale > 0.f ? logit_scale : 1.f;
-  return launch_token_logprobs(a, cut.per_thread, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEXT_OK : SPECEXT_ERR_LAUNCH_FAILED;
+  return launch_token_logprobs(a, cut.vectors, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEXT_OK : SPECEXT_ERR_LAUNCH_FAILED;
 }
 
 }  // extern "C"

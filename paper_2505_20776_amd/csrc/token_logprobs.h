@@ -23,19 +23,24 @@ struct LogprobArgs {
 constexpr int kLogprobThreads = 512;
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxTop = 64;
+constexpr int kMaxSlices = 64;
+constexpr int kLogprobWorkgroups = 512;      // smaller slices while there would be fewer
 
-// Values per thread (8, 16, 32 or 64) and slices of a row of `vocab` values.  A row's first address may lie up to seven values
+// 16-byte vectors per thread (1, 2, 4 or 8) and slices of a row of `vocab` values.  A row's first address may lie up to seven values
 // behind a multiple of 16 bytes, which the slices have to cover too.
 struct LogprobCut {
-  int per_thread, slices;
+  int vectors, slices;
 };
-inline LogprobCut logprob_cut(int vocab) {
-  const int values = vocab + 7;
-  int per_thread = 8;
-  while (per_thread < 64 && per_thread * kLogprobThreads < values) per_thread *= 2;
-  return {per_thread, (values + per_thread * kLogprobThreads - 1) / (per_thread * kLogprobThreads)};
+inline LogprobCut logprob_cut(int n_rows, int vocab, bool bf16) {
+  const int per_vector = bf16 ? 8 : 4;
+  const int values = vocab + per_vector - 1;
+  auto slices_of = [&](int vectors) { return (values + vectors * per_vector * kLogprobThreads - 1) / (vectors * per_vector * kLogprobThreads); };
+  int vectors = 8;
+  while (vectors > 1 && static_cast<int64_t>(n_rows) * slices_of(vectors) < kLogprobWorkgroups) vectors /= 2;
+  while (vectors < 8 && slices_of(vectors) > kMaxSlices) vectors *= 2;
+  return {vectors, slices_of(vectors)};
 }
 
-hipError_t launch_token_logprobs(const LogprobArgs& a, int per_thread, hipStream_t stream);
+hipError_t launch_token_logprobs(const LogprobArgs& a, int vectors, hipStream_t stream);
 
 }  // namespace specext

@@ -1,16 +1,19 @@
 // What a verification step reads from a row of logits: the most probable tokens (the first of them is the token that greedy
 // acceptance wants), the log-sum-exp, the entropy, and the log probabilities of given tokens.
 //
-//   x = logit_scale l;  lse = m + ln Z,  Z = sum e^(x - m);  entropy = ln Z - (sum e^(x - m) (x - m)) / Z;  log p(t) = (x_t - m) - ln Z
+//   m = max l,  t = e^(s (l - m)),  Z = sum t,  lse = s m + ln Z,  entropy = ln Z - s (sum t (l - m)) / Z,
+//   log p(i) = s (l_i - m) - ln Z                         (s = logit_scale)
 //
-// The logits are read once: a workgroup holds a slice of a row (512 threads x up to 64 values) in registers, so that the maximum
-// is known before the exponentials, and m is the slice's.  Long rows are several slices, joined by a second launch.
+// Bound by memory for many rows, by latency for few.  The logits are read once: a workgroup holds a slice of a row (512 threads x up
+// to eight 16-byte vectors) in registers, bf16 as it came, so that the maximum is known before the exponentials.  Long rows are
+// several slices, joined by a second launch.
 //
-// The k largest of a slice: a value and its index make one 64-bit key (larger values first, the lower index among equal ones),
-// so all keys differ and every answer is unique.  Each group of eight lanes finds its largest key; the k-th largest of these 64
-// keys has at least k keys at or above it, and few more: 20 of 32768 random values for k = 16.  Those are listed in LDS, and a
-// key whose rank in the list is r goes to place r.  A list that would overflow (values that crowd in few groups) has its
-// threshold raised by bisection first.
+// The k largest of a slice: a value and its index make one 64-bit key (larger values first, the lower index among equal ones), so all
+// keys differ and every answer is unique.  Each group of eight lanes has its largest value, which the softmax needs anyway; at or
+// above the k-th largest of these 64 are at least k values, and few more: 20 of 32768 random ones for k = 16.  Those are listed in
+// LDS, found through the maxima of the vectors, and a key whose rank in the list is r goes to place r.  Values that crowd (equal
+// ones, banned ones among the k best, a run of large ones in one group) overflow the list; the threshold is then the k-th largest of
+// the 512 threads' own best keys, and if that is not enough found by bisection.
 #include "mfma_util.h"
 #include "token_logprobs.h"
 
@@ -21,6 +24,7 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kList = 1024;             // keys that the list of a slice holds
 constexpr int kJoinThreads = 256;
+constexpr float kLargest = 3.402823466e38f;
 
 using Key = unsigned long long;
 
@@ -43,29 +47,29 @@ __device__ __forceinline__ Key key_from_lane(Key k, int mask) {
 }
 
 struct RowStats {
-  float m, z, w;      // maximum, sum of e^(x - m), sum of e^(x - m) (x - m)
+  float m, z, w;      // maximum, sum of t, sum of t (l - m)
 };
 
 // the last step: what the caller asked for of one row, from its sums and its k best keys in LDS
 __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, RowStats s, const Key* best, int n_best, int tid, int threads) {
   const bool empty = s.m == -INFINITY && s.z == 0.f;       // nothing but minus infinity
   const float ln_z = logf(s.z);
-  const float lse = empty ? -INFINITY : s.m + ln_z;
   if (tid == 0) {
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = empty ? 0.f : ln_z - s.w / s.z;
+    if (a.lse) a.lse[row] = empty ? -INFINITY : fmaf(a.logit_scale, s.m, ln_z);
+    if (a.entropy) a.entropy[row] = empty ? 0.f : ln_z - a.logit_scale * (s.w / s.z);
   }
   for (int i = tid; i < n_best; i += threads) {
     const float x = from_order_bits(static_cast<uint32_t>(best[i] >> 32));
     a.top_id[static_cast<int64_t>(row) * a.k + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(best[i]));
-    if (a.top_logprob) a.top_logprob[static_cast<int64_t>(row) * a.k + i] = empty ? -INFINITY : (x - s.m) - ln_z;
+    if (a.top_logprob) a.top_logprob[static_cast<int64_t>(row) * a.k + i] = empty ? -INFINITY : fmaf(a.logit_scale, x - s.m, -ln_z);
   }
   for (int i = tid; i < a.n_given; i += threads) {
     const int token = a.tokens[static_cast<int64_t>(row) * a.n_given + i];
     float lp = -INFINITY;                         // no token of the vocabulary
     if (token >= 0 && token < a.vocab && !empty) {
       const int64_t at = row * a.row_stride + token;
-      lp = ((a.bf16 ? bf16_bits_to_float(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at]) * a.logit_scale - s.m) - ln_z;
+      const float x = a.bf16 ? bf16_bits_to_float(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at];
+      lp = fmaf(a.logit_scale, x - s.m, -ln_z);
     }
     a.logprob[static_cast<int64_t>(row) * a.n_given + i] = lp;
   }
@@ -81,14 +85,14 @@ __device__ __forceinline__ void rank_keys(const Key* list, int n, int k, Key* ou
   }
 }
 
-// One slice of one row.  E values per thread; slice `s` holds the 16-byte vectors [s, s + 1) x kThreads x (E / V) of the row, counted
-// from the row's first address rounded down to 16 bytes.
-template <bool BF16, int E, bool ONE>
+// One slice of one row: N 16-byte vectors per thread.  Slice i holds the vectors [i, i + 1) x kThreads x N of the row, counted from the
+// row's first address rounded down to 16 bytes.
+template <bool BF16, int N, bool ONE>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   constexpr int V = BF16 ? 8 : 4;                 // values per vector
-  constexpr int N = E / V;
+  constexpr int kBytes = BF16 ? 2 : 4;
   __shared__ float part[3][kWaves];
-  __shared__ Key group_best[64];
+  __shared__ float group_top[64];
   __shared__ Key list[kList];
   __shared__ Key best[64];
   __shared__ int counts[kWaves];
@@ -96,71 +100,83 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = ONE ? blockIdx.x : blockIdx.x / a.slices;
   const int slice = ONE ? 0 : blockIdx.x - row * a.slices;
-  const unsigned char* base = static_cast<const unsigned char*>(a.logits) + row * a.row_stride * (BF16 ? 2 : 4);
-  const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(base) & 15) / (BF16 ? 2 : 4);   // values in front of the row in its first vector
-  base -= lead * (BF16 ? 2 : 4);
+  const unsigned char* base = static_cast<const unsigned char*>(a.logits) + row * a.row_stride * kBytes;
+  const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(base) & 15) / kBytes;   // values in front of the row in its first vector
+  base -= lead * kBytes;
 
-  // first[i]: index of vector i's first value; values outside [0, vocab) are absent
-  float x[E];
+  // values of a vector that lie outside the row are minus infinity here, and are told apart by their index where that matters
+  uintx4 w[N];
   auto first_of = [&](int i) { return (slice * N * kThreads + i * kThreads + tid) * V - lead; };
+  auto value = [&](const uintx4& v, int e) {
+    return BF16 ? __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16) : __uint_as_float(v[e & 3]);
+  };
+  // widened values and keys are made anew in every pass, instead of kept in as many registers again
+  auto forget = [&](uintx4& v) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+    for (int c = 0; c < 4; ++c) {
+      uint32_t u = v[c];
+      asm volatile("" : "+v"(u));
+      v[c] = u;
+    }
+  };
+  auto in_row = [&](int index) { return index >= 0 && index < a.vocab; };
+  auto load_vector = [&](int i) {
     const int first = first_of(i);
-    const unsigned char* at = base + static_cast<int64_t>(first + lead) * (BF16 ? 2 : 4);
-    if (first >= 0 && first + V <= a.vocab) {
-      const uintx4 w = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(at));
+    const unsigned char* at = base + static_cast<int64_t>(first + lead) * kBytes;
+    if (first >= 0 && first + V <= a.vocab) return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(at));
+    uint32_t u[4] = {};
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        x[i * V + e] = BF16 ? __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16) : __uint_as_float(w[e & 3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        x[i * V + e] = -INFINITY;
-        if (first + e >= 0 && first + e < a.vocab)
-          x[i * V + e] = BF16 ? bf16_bits_to_float(reinterpret_cast<const uint16_t*>(at)[e]) : reinterpret_cast<const float*>(at)[e];
+    for (int e = 0; e < V; ++e) {
+      if constexpr (BF16) {
+        const uint32_t x = in_row(first + e) ? reinterpret_cast<const uint16_t*>(at)[e] : 0xff80u;
+        u[e >> 1] |= x << (16 * (e & 1));
+      } else {
+        u[e] = in_row(first + e) ? reinterpret_cast<const uint32_t*>(at)[e] : 0xff800000u;
       }
     }
-  }
-  float top = -INFINITY;
+    return uintx4{u[0], u[1], u[2], u[3]};
+  };
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    x[e] *= a.logit_scale;
-    top = fmaxf(top, x[e]);
+  for (int i = 0; i < N; ++i) {
+    // all 512 vectors inside the row: no lane looks at its own place
+    const int first = (slice * N + i) * kThreads * V - lead;
+    if (__builtin_expect(first >= 0 && first + kThreads * V <= a.vocab, 1))
+      w[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(base + static_cast<int64_t>(first_of(i) + lead) * kBytes));
+    else
+      w[i] = load_vector(i);
   }
-  top = wave_max(top);
-  if (lane == 0) part[0][wave] = top;
+  const int k = a.k;
   if (tid == 0) listed = 0;
   if (tid < 64) best[tid] = 0;
-
-  // this thread's largest key, then its group's
-  const int k = a.k;
-  Key mine = 0;
-  if (k > 0) {
+  float top[N];                                   // of each vector
+  float mine = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+  for (int i = 0; i < N; ++i) {
+    top[i] = value(w[i], 0);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int index = first_of(i) + e;
-        const Key key = make_key(x[i * V + e], index);
-        if (index >= 0 && index < a.vocab) mine = max_key(mine, key);
-      }
-#pragma unroll
-    for (int m = 1; m < 8; m <<= 1) mine = max_key(mine, key_from_lane(mine, m));
-    if ((lane & 7) == 0) group_best[tid >> 3] = mine;
+    for (int e = 1; e < V; ++e) top[i] = fmaxf(top[i], value(w[i], e));
+    mine = fmaxf(mine, top[i]);
   }
+  mine = fmaxf(mine, SPECEXT_DPP(mine, 0xB1));    // of a group of eight lanes
+  mine = fmaxf(mine, SPECEXT_DPP(mine, 0x4E));
+  mine = fmaxf(mine, SPECEXT_DPP(mine, 0x141));
+  if ((lane & 7) == 0) group_top[tid >> 3] = mine;
   __syncthreads();
-  RowStats st;
-  st.m = part[0][0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) st.m = fmaxf(st.m, part[0][w]);
+  const float group = group_top[lane];
+  RowStats st = {wave_max(group), 0.f, 0.f};
   const float m = st.m == -INFINITY ? 0.f : st.m;
+  const float to_log2 = a.logit_scale * kLog2e;
   float z = 0.f, wsum = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float d = x[e] - m;
-    const float t = fast_exp2(d * kLog2e);
-    z += t;
-    wsum = fmaf(t, d < -1e4f ? -1e4f : d, wsum);    // 0 x -inf is 0 here; a NaN stays
+  for (int i = 0; i < N; ++i) {
+    forget(w[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float d = value(w[i], e) - m;
+      const float t = fast_exp2(d * to_log2);
+      z += t;
+      wsum = fmaf(t, d < -kLargest ? -kLargest : d, wsum);      // nothing times minus infinity is nothing here; a NaN stays
+    }
   }
   z = wave_sum(z);
   wsum = wave_sum(wsum);
@@ -168,64 +184,96 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
     part[1][wave] = z;
     part[2][wave] = wsum;
   }
-
   if (k > 0) {
-    // threshold: the k-th largest of the 64 group keys (0, every key, where fewer groups have any)
-    const Key own = group_best[lane];
-    int rank = 0;
-    for (int j = 0; j < 64; ++j) rank += group_best[j] > own ? 1 : 0;
-    const unsigned long long at_k = __ballot(rank == k - 1 && own != 0);
-    Key threshold = 0;
-    if (at_k) {
-      const int from = __builtin_ctzll(at_k);
-      threshold = group_best[from];
-    }
-    auto count_from = [&](Key from) {
-      int n = 0;
+    // the largest value that k groups reach
+    int reach = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
+    const float threshold = wave_max(reach >= k ? group : -INFINITY);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (top[i] >= threshold) {
+        forget(w[i]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float x = value(w[i], e);
+          const int index = first_of(i) + e;
+          if (x >= threshold && in_row(index)) {
+            const int at = atomicAdd(&listed, 1);
+            if (at < kList) list[at] = make_key(x, index);
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    st.z += part[1][v];
+    st.w += part[2][v];
+  }
+  if (k > 0) {
+    if (__builtin_expect(listed > kList || st.z != st.z, 0)) {
+      // too many, or a NaN, which no maximum shows: by keys, from the slice as it is in memory
+      auto count_from = [&](Key from) {
+        int n = 0;
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+          const uintx4 v = load_vector(i);
+#pragma unroll
+          for (int e = 0; e < V; ++e) n += in_row(first_of(i) + e) && make_key(value(v, e), first_of(i) + e) >= from ? 1 : 0;
+        }
+        n = static_cast<int>(wave_sum(static_cast<float>(n)));      // at most 4096: exact
+        __syncthreads();
+        if (lane == 0) counts[wave] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) n += counts[v];
+        return n;
+      };
+      Key own = 0;
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        const uintx4 v = load_vector(i);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (in_row(first_of(i) + e)) own = max_key(own, make_key(value(v, e), first_of(i) + e));
+      }
+      __syncthreads();
+      list[tid] = own;
+      if (tid == 0) list[kThreads] = 0;           // the threshold: 0, every key, where fewer than k threads have any
+      __syncthreads();
+      int rank = 0;
+      for (int j = 0; j < kThreads; ++j) rank += list[j] > own ? 1 : 0;
+      if (rank == k - 1 && own != 0) list[kThreads] = own;
+      __syncthreads();
+      Key lo = list[kThreads], hi = ~Key{0};
+      if (count_from(lo) > kList) {
+        // the largest threshold with at least k keys has exactly k
+        while (hi - lo > 1) {
+          const Key mid = lo + (hi - lo) / 2;
+          if (count_from(mid) >= k) lo = mid;
+          else hi = mid;
+        }
+      }
+      if (tid == 0) listed = 0;
+      __syncthreads();
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        const uintx4 v = load_vector(i);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const int index = first_of(i) + e;
-          n += index >= 0 && index < a.vocab && make_key(x[i * V + e], index) >= from ? 1 : 0;
+          const Key key = make_key(value(v, e), index);
+          if (in_row(index) && key >= lo) list[atomicAdd(&listed, 1)] = key;
         }
-      n = static_cast<int>(wave_sum(static_cast<float>(n)));      // at most 4096: exact
-      __syncthreads();
-      if (lane == 0) counts[wave] = n;
-      __syncthreads();
-      n = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) n += counts[w];
-      return n;
-    };
-    if (__builtin_expect(count_from(threshold) > kList, 0)) {
-      // the largest threshold with at least k keys has exactly k
-      Key lo = threshold, hi = ~Key{0};           // at least k keys from lo on, fewer than k from hi on
-      while (hi - lo > 1) {
-        const Key mid = lo + (hi - lo) / 2;
-        if (count_from(mid) >= k) lo = mid;
-        else hi = mid;
       }
-      threshold = lo;
+      __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int index = first_of(i) + e;
-        const Key key = make_key(x[i * V + e], index);
-        if (index >= 0 && index < a.vocab && key >= threshold) list[atomicAdd(&listed, 1)] = key;
-      }
+    rank_keys(list, listed, k, best, tid, kThreads);
+    __syncthreads();
   }
-  __syncthreads();
-  st.z = 0.f, st.w = 0.f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    st.z += part[1][w];
-    st.w += part[2][w];
-  }
-  if (k > 0) rank_keys(list, listed, k, best, tid, kThreads);
-  __syncthreads();
   if constexpr (ONE) {
     finish_row(a, row, st, best, k, tid, kThreads);
   } else {
@@ -250,9 +298,9 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
     const floatx4 t = *reinterpret_cast<const floatx4*>(a.stats + (static_cast<int64_t>(row) * a.slices + i) * 4);
     if (t[0] == -INFINITY && t[1] == 0.f) continue;         // nothing but minus infinity
     const float d = t[0] - s.m;
-    const float f = fast_exp2(d * kLog2e);
+    const float f = fast_exp2(d * a.logit_scale * kLog2e);
     s.z = fmaf(t[1], f, s.z);
-    s.w = fmaf(f, fmaf(d < -1e4f ? -1e4f : d, t[1], t[2]), s.w);
+    if (f > 0.f) s.w = fmaf(f, fmaf(d, t[1], t[2]), s.w);
   }
   __syncthreads();
   // short slices leave zeros behind their keys; every row has k keys at least, and zeros rank behind all of them
@@ -262,23 +310,22 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
 }
 
 template <bool BF16, bool ONE>
-hipError_t launch_slices(const LogprobArgs& a, int per_thread, hipStream_t stream) {
+hipError_t launch_slices(const LogprobArgs& a, int vectors, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(a.n_rows) * a.slices), block(kThreads);
-  switch (per_thread) {
-    case 8: return launch_kernel(logprobs_kernel<BF16, 8, ONE>, grid, block, 0, stream, a);
-    case 16: return launch_kernel(logprobs_kernel<BF16, 16, ONE>, grid, block, 0, stream, a);
-    case 32: return launch_kernel(logprobs_kernel<BF16, 32, ONE>, grid, block, 0, stream, a);
-    default: return launch_kernel(logprobs_kernel<BF16, 64, ONE>, grid, block, 0, stream, a);
+  switch (vectors) {
+    case 1: return launch_kernel(logprobs_kernel<BF16, 1, ONE>, grid, block, 0, stream, a);
+    case 2: return launch_kernel(logprobs_kernel<BF16, 2, ONE>, grid, block, 0, stream, a);
+    case 4: return launch_kernel(logprobs_kernel<BF16, 4, ONE>, grid, block, 0, stream, a);
+    default: return launch_kernel(logprobs_kernel<BF16, 8, ONE>, grid, block, 0, stream, a);
   }
 }
 
 }  // namespace
 
-hipError_t launch_token_logprobs(const LogprobArgs& a, int per_thread, hipStream_t stream) {
+hipError_t launch_token_logprobs(const LogprobArgs& a, int vectors, hipStream_t stream) {
   if (a.n_rows <= 0) return hipSuccess;
-  hipError_t e;
-  if (a.slices == 1) return a.bf16 ? launch_slices<true, true>(a, per_thread, stream) : launch_slices<false, true>(a, per_thread, stream);
-  e = a.bf16 ? launch_slices<true, false>(a, per_thread, stream) : launch_slices<false, false>(a, per_thread, stream);
+  if (a.slices == 1) return a.bf16 ? launch_slices<true, true>(a, vectors, stream) : launch_slices<false, true>(a, vectors, stream);
+  const hipError_t e = a.bf16 ? launch_slices<true, false>(a, vectors, stream) : launch_slices<false, false>(a, vectors, stream);
   if (e != hipSuccess) return e;
   const int lds_bytes = (a.slices + 1) * a.k * static_cast<int>(sizeof(Key));
   return launch_kernel(logprobs_join_kernel, dim3(a.n_rows), dim3(kJoinThreads), lds_bytes, stream, a);
