@@ -9,11 +9,11 @@
 // several slices, joined by a second launch.
 //
 // The k largest of a slice: a value and its index make one 64-bit key (larger values first, the lower index among equal ones), so all
-// keys differ and every answer is unique.  Each group of eight lanes has its largest value, which the softmax needs anyway; at or
-// above the k-th largest of these 64 are at least k values, and few more: 20 of 32768 random ones for k = 16.  Those are listed in
-// LDS, found through the maxima of the vectors, and a key whose rank in the list is r goes to place r.  Values that crowd (equal
-// ones, banned ones among the k best, a run of large ones in one group) overflow the list; the threshold is then the k-th largest of
-// the 512 threads' own best keys, and if that is not enough found by bisection.
+// keys differ and every answer is unique.  Each wave, or for more than eight answers each group of eight lanes, has its largest value,
+// which the softmax needs anyway; at or above the k-th largest of these are at least k values, and few more: about 20 of 32768 random
+// ones for k = 8, and for k = 16.  Those are listed in LDS, found through the maxima of the vectors, and a key whose rank in the list is r goes to place r.  Values that crowd (many
+// equal ones, a run of large ones in one group) overflow the list; the threshold is then the k-th largest of the 512 threads' own
+// best keys, and if that is not enough found by bisection.
 #include "mfma_util.h"
 #include "token_logprobs.h"
 
@@ -75,12 +75,25 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, RowSta
   }
 }
 
-// ranks of `n` keys in LDS, all different; the k largest to out in order
-__device__ __forceinline__ void rank_keys(const Key* list, int n, int k, Key* out, int tid, int threads) {
+// The k largest of n keys in LDS, all different, to out in order.  The list has room for kRankStep keys more, which are cleared here:
+// the comparisons read whole steps, all their reads under way at once.
+constexpr int kRankStep = 16;
+template <bool ONE_WAVE = false>
+__device__ __forceinline__ void rank_keys(Key* list, int n, int k, Key* out, int tid, int threads) {
+  typedef __attribute__((ext_vector_type(2))) Key Key2;
+  if (tid < kRankStep) list[n + tid] = 0;
+  if (ONE_WAVE) __builtin_amdgcn_wave_barrier();
+  else __syncthreads();
   for (int i = tid; i < n; i += threads) {
     const Key mine = list[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
+    for (int j = 0; j < n; j += kRankStep) {
+      Key2 other[kRankStep / 2];
+#pragma unroll
+      for (int u = 0; u < kRankStep / 2; ++u) other[u] = reinterpret_cast<const Key2*>(list + j)[u];
+#pragma unroll
+      for (int u = 0; u < kRankStep / 2; ++u) rank += (other[u][0] > mine ? 1 : 0) + (other[u][1] > mine ? 1 : 0);
+    }
     if (rank < k) out[rank] = mine;
   }
 }
@@ -91,9 +104,10 @@ template <bool BF16, int N, bool ONE>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   constexpr int V = BF16 ? 8 : 4;                 // values per vector
   constexpr int kBytes = BF16 ? 2 : 4;
-  __shared__ float part[3][kWaves];
+  __shared__ float part[2][kWaves];
   __shared__ float group_top[64];
-  __shared__ Key list[kList];
+  __shared__ float threshold_of;
+  __shared__ __attribute__((aligned(16))) Key list[kList + kRankStep];
   __shared__ Key best[64];
   __shared__ int counts[kWaves];
   __shared__ int listed;
@@ -157,13 +171,34 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
     for (int e = 1; e < V; ++e) top[i] = fmaxf(top[i], value(w[i], e));
     mine = fmaxf(mine, top[i]);
   }
-  mine = fmaxf(mine, SPECEXT_DPP(mine, 0xB1));    // of a group of eight lanes
+  // the largest value of each group: for up to eight answers a group is a wave, else eight lanes
+  const bool few = k <= kWaves;
+  mine = fmaxf(mine, SPECEXT_DPP(mine, 0xB1));
   mine = fmaxf(mine, SPECEXT_DPP(mine, 0x4E));
   mine = fmaxf(mine, SPECEXT_DPP(mine, 0x141));
-  if ((lane & 7) == 0) group_top[tid >> 3] = mine;
+  if (few) {
+    mine = wave_max(mine);
+    if (lane == 0) group_top[wave] = mine;
+  } else if ((lane & 7) == 0) {
+    group_top[tid >> 3] = mine;
+  }
   __syncthreads();
-  const float group = group_top[lane];
+  const float group = group_top[few ? lane & (kWaves - 1) : lane];
   RowStats st = {wave_max(group), 0.f, 0.f};
+  // the threshold: the largest value that k groups reach
+  float threshold = st.m;
+  if (few) {
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
+    threshold = wave_max(reach >= k ? group : -INFINITY);
+  } else if (wave == 0) {                         // while the other waves take exponentials
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
+    const float reached = wave_max(reach >= k ? group : -INFINITY);
+    if (lane == 0) threshold_of = reached;
+  }
   const float m = st.m == -INFINITY ? 0.f : st.m;
   const float to_log2 = a.logit_scale * kLog2e;
   float z = 0.f, wsum = 0.f;
@@ -175,21 +210,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
       const float d = value(w[i], e) - m;
       const float t = fast_exp2(d * to_log2);
       z += t;
-      wsum = fmaf(t, d < -kLargest ? -kLargest : d, wsum);      // nothing times minus infinity is nothing here; a NaN stays
+      wsum = fmaf(t, fmaxf(d, -kLargest), wsum);          // nothing times minus infinity is nothing here; t of a NaN is one
     }
   }
   z = wave_sum(z);
   wsum = wave_sum(wsum);
   if (lane == 0) {
-    part[1][wave] = z;
-    part[2][wave] = wsum;
+    part[0][wave] = z;
+    part[1][wave] = wsum;
+  }
+  if (!few) {
+    __syncthreads();
+    threshold = threshold_of;
   }
   if (k > 0) {
-    // the largest value that k groups reach
-    int reach = 0;
-#pragma unroll
-    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
-    const float threshold = wave_max(reach >= k ? group : -INFINITY);
+    // Fewer than k groups with anything but minus infinity: everything else there is, and the first k values of the slice, among
+    // which are as many of the minus infinities as are wanted, of the lowest indices.
+    const int slice_first = slice * N * kThreads * V - lead;
+    const int equal_end = threshold == -INFINITY ? (slice_first < 0 ? 0 : slice_first) + k : 0x7fffffff;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (top[i] >= threshold) {
@@ -197,10 +235,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float x = value(w[i], e);
-          const int index = first_of(i) + e;
-          if (x >= threshold && in_row(index)) {
-            const int at = atomicAdd(&listed, 1);
-            if (at < kList) list[at] = make_key(x, index);
+          if (x >= threshold) {
+            const int index = first_of(i) + e;
+            if ((x > threshold || index < equal_end) && in_row(index)) {
+              const int place = atomicAdd(&listed, 1);
+              if (place < kList) list[place] = make_key(x, index);
+            }
           }
         }
       }
@@ -209,8 +249,22 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   __syncthreads();
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) {
-    st.z += part[1][v];
-    st.w += part[2][v];
+    st.z += part[0][v];
+    st.w += part[1][v];
+  }
+  const int64_t at = ONE ? row : static_cast<int64_t>(row) * a.slices + slice;
+  if (__builtin_expect(listed <= 128 && st.z == st.z, 1)) {
+    // a short list, as a rule: one wave ranks it, the others leave their place to the next workgroup
+    if (wave != 0) return;
+    if (k > 0) rank_keys<true>(list, listed, k, best, lane, 64);
+    __builtin_amdgcn_wave_barrier();
+    if constexpr (ONE) {
+      finish_row(a, row, st, best, k, lane, 64);
+    } else {
+      if (lane == 0) *reinterpret_cast<floatx4*>(a.stats + at * 4) = floatx4{st.m, st.z, st.w, 0.f};
+      if (lane < k) a.keys[at * k + lane] = best[lane];
+    }
+    return;
   }
   if (k > 0) {
     if (__builtin_expect(listed > kList || st.z != st.z, 0)) {
@@ -242,13 +296,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
       }
       __syncthreads();
       list[tid] = own;
-      if (tid == 0) list[kThreads] = 0;           // the threshold: 0, every key, where fewer than k threads have any
       __syncthreads();
-      int rank = 0;
-      for (int j = 0; j < kThreads; ++j) rank += list[j] > own ? 1 : 0;
-      if (rank == k - 1 && own != 0) list[kThreads] = own;
+      // (best holds zeros: the threshold is 0, every key, where fewer than k threads have any)
+      rank_keys(list, kThreads, k, best, tid, kThreads);
       __syncthreads();
-      Key lo = list[kThreads], hi = ~Key{0};
+      Key lo = best[k - 1], hi = ~Key{0};
       if (count_from(lo) > kList) {
         // the largest threshold with at least k keys has exactly k
         while (hi - lo > 1) {
@@ -257,7 +309,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
           else hi = mid;
         }
       }
+      __syncthreads();
       if (tid == 0) listed = 0;
+      if (tid < 64) best[tid] = 0;
       __syncthreads();
 #pragma unroll 1
       for (int i = 0; i < N; ++i) {
@@ -277,34 +331,32 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   if constexpr (ONE) {
     finish_row(a, row, st, best, k, tid, kThreads);
   } else {
-    const int64_t at = static_cast<int64_t>(row) * a.slices + slice;
     if (tid == 0) *reinterpret_cast<floatx4*>(a.stats + at * 4) = floatx4{st.m, st.z, st.w, 0.f};
     if (tid < k) a.keys[at * k + tid] = best[tid];
   }
 }
 
-// the slices of one row
+// The slices of one row: a lane has one of them.
 __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  Key* list = reinterpret_cast<Key*>(lds);        // slices x k, then k best
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int row = blockIdx.x;
   const int n = a.slices * a.k;
-  Key* best = list + n;
+  Key* list = reinterpret_cast<Key*>(lds);        // n keys, kRankStep more, then the k best
+  Key* best = list + n + kRankStep;
+  static_assert(kMaxSlices <= 64, "a slice per lane");
+  floatx4 t = {-INFINITY, 0.f, 0.f, 0.f};
+  if (lane < a.slices) t = *reinterpret_cast<const floatx4*>(a.stats + (static_cast<int64_t>(row) * a.slices + lane) * 4);
   for (int i = tid; i < n; i += kJoinThreads) list[i] = a.keys[static_cast<int64_t>(row) * n + i];
-  RowStats s = {-INFINITY, 0.f, 0.f};
-  for (int i = 0; i < a.slices; ++i) s.m = fmaxf(s.m, a.stats[(static_cast<int64_t>(row) * a.slices + i) * 4]);
-  for (int i = 0; i < a.slices; ++i) {
-    const floatx4 t = *reinterpret_cast<const floatx4*>(a.stats + (static_cast<int64_t>(row) * a.slices + i) * 4);
-    if (t[0] == -INFINITY && t[1] == 0.f) continue;         // nothing but minus infinity
-    const float d = t[0] - s.m;
-    const float f = fast_exp2(d * a.logit_scale * kLog2e);
-    s.z = fmaf(t[1], f, s.z);
-    if (f > 0.f) s.w = fmaf(f, fmaf(d, t[1], t[2]), s.w);
-  }
-  __syncthreads();
+  RowStats s;
+  s.m = wave_max(t[0]);
+  // a slice of nothing but minus infinity adds nothing (nor does it where the whole row is that)
+  const float d = t[0] == s.m ? 0.f : t[0] - s.m;
+  const float f = fast_exp2(d * a.logit_scale * kLog2e);
+  s.z = wave_sum(t[1] * f);
+  s.w = wave_sum(f > 0.f ? f * fmaf(d, t[1], t[2]) : 0.f);
   // short slices leave zeros behind their keys; every row has k keys at least, and zeros rank behind all of them
-  rank_keys(list, n, a.k, best, tid, kJoinThreads);
+  if (a.k > 0) rank_keys(list, n, a.k, best, tid, kJoinThreads);
   __syncthreads();
   finish_row(a, row, s, best, a.k, tid, kJoinThreads);
 }
@@ -327,7 +379,7 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, int vectors, hipStream_t 
   if (a.slices == 1) return a.bf16 ? launch_slices<true, true>(a, vectors, stream) : launch_slices<false, true>(a, vectors, stream);
   const hipError_t e = a.bf16 ? launch_slices<true, false>(a, vectors, stream) : launch_slices<false, false>(a, vectors, stream);
   if (e != hipSuccess) return e;
-  const int lds_bytes = (a.slices + 1) * a.k * static_cast<int>(sizeof(Key));
+  const int lds_bytes = ((a.slices + 1) * a.k + kRankStep) * static_cast<int>(sizeof(Key));
   return launch_kernel(logprobs_join_kernel, dim3(a.n_rows), dim3(kJoinThreads), lds_bytes, stream, a);
 }
 
