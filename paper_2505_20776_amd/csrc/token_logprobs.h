@@ -24,7 +24,9 @@ constexpr int kLogprobThreads = 512;
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxTop = 64;
 constexpr int kMaxSlices = 64;
-constexpr int kLogprobWorkgroups = 512;      // smaller slices while there would be fewer
+// Slices are made smaller while there would be fewer than 128 workgroups.  us with 128 / 512, bf16 rows of 128256: 20 rows 9.1 / 9.8, 60 10.3 /
+// 10.8; 60 fp32 rows of 32000 8.9 / 10.8; equal from 128 rows on and for one row.
+constexpr int kLogprobWorkgroups = 128;
 
 // 16-byte vectors per thread (1, 2, 4 or 8) and slices of a row of `vocab` values.  A row's first address may lie up to seven values
 // behind a multiple of 16 bytes, which the slices have to cover too.

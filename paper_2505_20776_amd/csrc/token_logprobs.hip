@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   constexpr int V = BF16 ? 8 : 4;                 // values per vector
   constexpr int kBytes = BF16 ? 2 : 4;
   __shared__ float part[2][kWaves];
-  __shared__ float group_top[64];
+  __shared__ float group_top[64], wave_top[kWaves];
   __shared__ float threshold_of;
   __shared__ __attribute__((aligned(16))) Key list[kList + kRankStep];
   __shared__ Key best[64];
@@ -171,32 +171,35 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
     for (int e = 1; e < V; ++e) top[i] = fmaxf(top[i], value(w[i], e));
     mine = fmaxf(mine, top[i]);
   }
-  // the largest value of each group: for up to eight answers a group is a wave, else eight lanes
-  const bool few = k <= kWaves;
+  // the largest values of eight lanes and of the wave
   mine = fmaxf(mine, SPECEXT_DPP(mine, 0xB1));
   mine = fmaxf(mine, SPECEXT_DPP(mine, 0x4E));
   mine = fmaxf(mine, SPECEXT_DPP(mine, 0x141));
-  if (few) {
-    mine = wave_max(mine);
-    if (lane == 0) group_top[wave] = mine;
-  } else if ((lane & 7) == 0) {
-    group_top[tid >> 3] = mine;
-  }
+  if ((lane & 7) == 0) group_top[tid >> 3] = mine;
+  mine = wave_max(mine);
+  if (lane == 0) wave_top[wave] = mine;
   __syncthreads();
-  const float group = group_top[few ? lane & (kWaves - 1) : lane];
-  RowStats st = {wave_max(group), 0.f, 0.f};
-  // the threshold: the largest value that k groups reach
+  const float of_wave = wave_top[lane & (kWaves - 1)];
+  RowStats st = {wave_max(of_wave), 0.f, 0.f};
+  // The threshold: the largest value that k groups reach.  For up to eight answers a group is a wave, unless too few waves have
+  // values (a short slice); else eight lanes, found by one wave while the others take exponentials.
+  auto of_groups = [&]() __attribute__((always_inline)) {
+    const float group = group_top[lane];
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
+    return wave_max(reach >= k ? group : -INFINITY);
+  };
+  const bool few = k <= kWaves;
   float threshold = st.m;
   if (few) {
     int reach = 0;
 #pragma unroll
-    for (int j = 0; j < kWaves; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
-    threshold = wave_max(reach >= k ? group : -INFINITY);
-  } else if (wave == 0) {                         // while the other waves take exponentials
-    int reach = 0;
-#pragma unroll
-    for (int j = 0; j < 64; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j)) >= group ? 1 : 0;
-    const float reached = wave_max(reach >= k ? group : -INFINITY);
+    for (int j = 0; j < kWaves; ++j) reach += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of_wave), j)) >= of_wave ? 1 : 0;
+    threshold = wave_max(reach >= k ? of_wave : -INFINITY);
+    if (__builtin_expect(threshold == -INFINITY && k > 0, 0)) threshold = of_groups();
+  } else if (wave == 0) {
+    const float reached = of_groups();
     if (lane == 0) threshold_of = reached;
   }
   const float m = st.m == -INFINITY ? 0.f : st.m;

@@ -194,3 +194,11 @@ def test_captured_and_replayed_on_a_side_stream():
         call()
         torch.cuda.synchronize()
         assert torch.equal(ids, eager[0])
+
+
+@pytest.mark.parametrize("dtype,vocab", [(torch.bfloat16, 1280), (torch.bfloat16, 12 * 4096 + 1280), (torch.float32, 700), (torch.bfloat16, 65), (torch.float32, 2048 * 9 + 300)])
+@pytest.mark.parametrize("k", [4, 8, 9])
+def test_slices_that_fill_few_waves(dtype, vocab, k):
+    """The last slice of a row has values for fewer waves than answers are wanted."""
+    x, _ = _logits(vocab + k, 5, vocab, dtype)
+    _check(x, k)
