@@ -132,7 +132,7 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   if (quant_block) {
     p->use_mfma = 4;
     p->rows_per_group = p->M <= 32 ? 32 : p->M <= 64 ? 64 : p->M <= 128 ? 128 : 256;
-    p->part_f16 = 0;
+    p->part_f16 = p->d == 128 && p->rows_per_group == 256;
   } else if (mfma64_ok) {
     p->use_mfma = 2;
     p->rows_per_group = p->M > 128 ? 256 : 128;

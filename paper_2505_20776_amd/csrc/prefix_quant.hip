@@ -29,11 +29,13 @@ constexpr int kTile = 32;      // keys per tile
 
 template <int D>
 __host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }      // K or V of a tile as fp16
+constexpr int kPatchStride = 128 * 2 + 8;       // a row of fp16 partials in LDS, padded against bank conflicts
+constexpr int kPatchBytes = 32 * kPatchStride;
 template <int D, int R, int KG>
 constexpr int lds_bytes() {
   const int buffers = 2 * KG * 2 * tile_bytes<D>();
-  const int merge = KG > 1 ? R * KG * (D * kTile * 4 + 2 * 32 * 4) : 0;
-  return buffers > merge ? buffers : merge;
+  const int end = KG > 1 ? R * KG * (D * kTile * 4 + 2 * 32 * 4) : D == 128 ? R * kPatchBytes : 0;
+  return buffers > end ? buffers : end;
 }
 
 // four e4m3 values -> fp16, exactly
@@ -87,47 +89,47 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   // ---- loads: this thread's 16-byte pieces of the tile of its key group
   const unsigned char* kbase = in_global<const unsigned char>(k_at) + g * kp_sh;
   const unsigned char* vbase = in_global<const unsigned char>(v_at) + g * kp_sh;
-  uintx4 raw[PF][kPiecesPerWave];
-  auto load_stage = [&](auto slot_c, int t) __attribute__((always_inline)) {
-    constexpr int slot = decltype(slot_c)::value;
-    const int key0 = key_lo + (t * KG + kg) * kTile;
-#pragma unroll
-    for (int i = 0; i < kPiecesPerWave; ++i) {
-      const int piece = i * R + r_block;
-      if (kPieces < R && piece >= kPieces) continue;
-      const bool is_v = piece >= kPieces / 2;
-      const int row = (is_v ? piece - kPieces / 2 : piece) * kPieceRows + lane / kLanesPerRow;
-      // keys behind the prefix: its last one again, masked below
-      const int64_t off = static_cast<int64_t>(min(key0 + row, L - 1)) * kp_sl + (lane % kLanesPerRow) * 16;
-      raw[slot][i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>((is_v ? vbase : kbase) + off));
-    }
+  // keys behind the prefix: its last one again, masked below
+  auto piece_is_v = [&](int i) { return i * R + r_block >= kPieces / 2; };
+  auto piece_row = [&](int i) { return (i * R + r_block) % (kPieces / 2) * kPieceRows + lane / kLanesPerRow; };
+  auto piece_there = [&](int i) { return kPieces >= R || i * R + r_block < kPieces; };
+  auto load_piece = [&](int i, int stage) {
+    const int key = min(key_lo + (stage * KG + kg) * kTile + piece_row(i), L - 1);
+    return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>((piece_is_v(i) ? vbase : kbase) + key * kp_sl + (lane % kLanesPerRow) * 16));
   };
-  // ---- LDS: per buffer and key group a K and a V tile of 32 rows.  The 16-byte chunks of a row are XOR-swizzled so that the
-  // operand reads are free of bank conflicts.
+  // ---- LDS: per key group two K and two V tiles of 32 rows.  The 16-byte chunks of a row are XOR-swizzled so that the operand
+  // reads are free of bank conflicts.
   auto k_swizzle = [](int row) { return D == 128 ? (row & 15) : ((row >> 1) & 7); };
   auto v_swizzle = [](int row) { return D == 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); };
-  auto store_stage = [&](auto slot_c, auto buf_c) __attribute__((always_inline)) {
-    constexpr int slot = decltype(slot_c)::value;
-    constexpr int buf = decltype(buf_c)::value;
+  auto store_piece = [&](int i, const uintx4& w, int buf) __attribute__((always_inline)) {
+    const int row = piece_row(i);
+    const int chunk = 2 * (lane % kLanesPerRow);
+    const int swizzle = piece_is_v(i) ? v_swizzle(row) : k_swizzle(row);
+    unsigned char* dst = lds + ((kg * 2 + buf) * 2 + (piece_is_v(i) ? 1 : 0)) * kTileBytes + row * kRowBytes;
+    uint32_t h[8];
 #pragma unroll
-    for (int i = 0; i < kPiecesPerWave; ++i) {
-      const int piece = i * R + r_block;
-      if (kPieces < R && piece >= kPieces) continue;
-      const bool is_v = piece >= kPieces / 2;
-      const int row = (is_v ? piece - kPieces / 2 : piece) * kPieceRows + lane / kLanesPerRow;
-      const int chunk = 2 * (lane % kLanesPerRow);
-      const int swizzle = is_v ? v_swizzle(row) : k_swizzle(row);
-      unsigned char* dst = lds + (buf * KG + kg) * 2 * kTileBytes + (is_v ? kTileBytes : 0) + row * kRowBytes;
-      uint32_t h[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) widen4(raw[slot][i][e], h + 2 * e);
-      *reinterpret_cast<uintx4*>(dst + ((chunk ^ swizzle) << 4)) = uintx4{h[0], h[1], h[2], h[3]};
-      *reinterpret_cast<uintx4*>(dst + (((chunk + 1) ^ swizzle) << 4)) = uintx4{h[4], h[5], h[6], h[7]};
-    }
+    for (int e = 0; e < 4; ++e) widen4(w[e], h + 2 * e);
+    *reinterpret_cast<uintx4*>(dst + ((chunk ^ swizzle) << 4)) = uintx4{h[0], h[1], h[2], h[3]};
+    *reinterpret_cast<uintx4*>(dst + (((chunk + 1) ^ swizzle) << 4)) = uintx4{h[4], h[5], h[6], h[7]};
   };
-  static_for<0, PF>([&](auto u_c) {
-    if (decltype(u_c)::value < n_stages) load_stage(u_c, decltype(u_c)::value);
-  });
+  // Logits are a stage ahead of their softmax, so K is a stage ahead of V: step t brings K of stage t + 1 and V of stage t.
+  uintx4 raw[PF][kPiecesPerWave];
+  auto load_step = [&](auto slot_c, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kPiecesPerWave; ++i)
+      if (piece_there(i)) raw[decltype(slot_c)::value][i] = load_piece(i, piece_is_v(i) ? t : t + 1);
+  };
+  auto store_step = [&](auto slot_c, auto v_buf_c) __attribute__((always_inline)) {
+    constexpr int v_buf = decltype(v_buf_c)::value;
+#pragma unroll
+    for (int i = 0; i < kPiecesPerWave; ++i)
+      if (piece_there(i)) store_piece(i, raw[decltype(slot_c)::value][i], piece_is_v(i) ? v_buf : 1 - v_buf);
+  };
+  uintx4 first_k[kPiecesPerWave];
+#pragma unroll
+  for (int i = 0; i < kPiecesPerWave; ++i)
+    if (piece_there(i) && !piece_is_v(i)) first_k[i] = load_piece(i, 0);
+  static_for<0, PF>([&](auto u_c) { load_step(u_c, decltype(u_c)::value); });
 
   // ---- queries: B operand of S^T (lane = row c32, 8 consecutive d per step), moved to 2^8 at the most
   halfx8 qf[kSteps];
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     c = __builtin_amdgcn_ldexpf(p.scale_log2, -shift);
   }
 
-  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)lds)) + kg * 2 * kTileBytes;
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)lds)) + kg * 4 * kTileBytes;
   unsigned k_addr[kSteps], v_addr[kBlocks];
 #pragma unroll
   for (int ks = 0; ks < kSteps; ++ks) k_addr[ks] = lds0 + c32 * kRowBytes + (((2 * ks + hf) ^ k_swizzle(c32)) << 4);
@@ -189,28 +191,26 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   const unsigned score_off = static_cast<unsigned>(min(row0 + c32, M - 1)) * 8u;
   if (SCORES) score_base = reinterpret_cast<unsigned char*>(p.chunk_part) + (static_cast<int64_t>(g) * p.n_sub + key_lo / kTile) * score_step;
 
-  auto compute = [&](int j, auto buf_c) __attribute__((always_inline)) {
-    constexpr int buf = decltype(buf_c)::value * KG * 2 * kTileBytes;
-    const int key0 = key_lo + j * kTile;
-    const float sk = k_scale[key0 >> block_log2];
-    const float sv = v_scale[key0 >> block_log2];
-    floatx16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // the tile whose softmax comes next
+  floatx16 s = {};
+  float sk = 0.f, sv = 0.f;      // and its scales
+  auto logits = [&](floatx16& x, auto buf_c) __attribute__((always_inline)) {
+    constexpr int buf = decltype(buf_c)::value * 2 * kTileBytes;
+    x = floatx16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < kSteps; ++ks) {
       const uintx4 kw = *reinterpret_cast<const lds_uintx4*>(static_cast<uintptr_t>(k_addr[ks] + buf));
-      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, kw), qf[ks], s, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, kw), qf[ks], x, 0, 0, 0);
     }
-    halfx8 vf[kBlocks][2];
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        const unsigned at = v_addr[db] + buf + 16 * jj * kRowBytes;
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at));
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at + 8 * kRowBytes));
-        vf[db][jj] = __builtin_bit_cast(halfx8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-    // register r of s holds key key0 + 8 (r / 4) + 4 hf + r % 4
+  };
+  auto scale_of = [&](const const_float* scale, int j) { return scale[min(key_lo + j * kTile, key_hi - 1) >> block_log2]; };
+  // Tile j from its logits in s on, and the logits of tile j + KG into the matrix pipe while the vector ALUs take the exponentials.
+  // (Behind the last tile those are of whatever the buffer holds, and nobody reads them: cheaper than a second form of the loop's
+  // body, whose registers would spill.)
+  auto tile = [&](int j, auto buf_c) __attribute__((always_inline)) {
+    constexpr int buf = decltype(buf_c)::value;
+    const int key0 = key_lo + j * kTile;
+    // register r holds key key0 + 8 (r / 4) + 4 hf + r % 4
     if (__builtin_expect(key0 + kTile > key_hi, 0)) {
       const int left = key_hi - key0 - 4 * hf;
 #pragma unroll
@@ -220,13 +220,13 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     const float ct = c * sk;
     const float lsv = __builtin_amdgcn_logf(sv);
     const float inv_sv = __builtin_amdgcn_rcpf(sv);
-    float mx = fmaxf(s[0], s[1]);
+    float top = fmaxf(s[0], s[1]);
 #pragma unroll
-    for (int r = 2; r < 16; r += 2) mx = fmaxf(mx, fmaxf(s[r], s[r + 1]));
-    mx = fmaf(mx, ct, lsv);
-    if (__builtin_expect(__any(mx > ref + kLazyLog2), 0)) {     // some row of this wave outgrew its reference: move every reference up
-      const float new_ref = fmaxf(ref, halves_max(mx));
-      const float alpha = fast_exp2(ref - new_ref);             // 0 on the first tile
+    for (int r = 2; r < 16; r += 2) top = fmaxf(top, fmaxf(s[r], s[r + 1]));
+    top = fmaf(top, ct, lsv);                                    // the row's largest, the values' scale included
+    if (__builtin_expect(__any(top > ref + kLazyLog2), 0)) {     // some row of this wave outgrew its reference: move every reference up
+      const float new_ref = fmaxf(ref, halves_max(top));
+      const float alpha = fast_exp2(ref - new_ref);              // 0 on the first tile
       ref = new_ref;
       run_sum *= alpha;
 #pragma unroll
@@ -234,6 +234,9 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc_o[db][r] *= alpha;
     }
+    sk = scale_of(k_scale, j + KG), sv = scale_of(v_scale, j + KG);
+    floatx16 next;
+    logits(next, ic<1 - buf>{});
     const float shift = lsv - ref;
     float part = 0.f;
 #pragma unroll
@@ -243,37 +246,115 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     }
     part *= inv_sv;
     run_sum += part;
+    asm volatile("" : "+v"(run_sum));        // here, not behind the next branch
     // every lane stores: the two lanes of a row hold the same pair, and so do padding rows
     if (SCORES) *reinterpret_cast<floatx2*>(score_base + j * score_step + score_off) = floatx2{halves_sum(part), ref};
     const halfx8 p0 = pack8_f16(s, 0), p1 = pack8_f16(s, 8);
+    __builtin_amdgcn_sched_group_barrier(0x100, kSteps, 0);         // LDS reads
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {                              // a matrix instruction, then its share of the exponentials
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 56 / kSteps, 0);
+    }
+    // The logits' last product stays in front of the second product: left to the compiler it sinks behind that, to the branch in front
+    // of the next maxima.  There it waits in the matrix pipe for the product before it, for longer than the compiler's distance to its
+    // first reader allows for, and that reader (two logits of a lane) now and then saw the sum of seven eighths of the row.
+    asm volatile("" : "+v"(next));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int db = 0; db < kBlocks; ++db) {
-      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[db][0], p0, acc_o[db], 0, 0, 0);
-      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[db][1], p1, acc_o[db], 0, 0, 0);
+      halfx8 vf[2];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        const unsigned at = v_addr[db] + buf * 2 * kTileBytes + 16 * jj * kRowBytes;
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at + 8 * kRowBytes));
+        vf[jj] = __builtin_bit_cast(halfx8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[0], p0, acc_o[db], 0, 0, 0);
+      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[1], p1, acc_o[db], 0, 0, 0);
     }
+    s = next;
+    __builtin_amdgcn_sched_barrier(0);
   };
 
-  // stage t lives in registers raw[t % PF], then in LDS buffer t % 2
-  store_stage(ic<0>{}, ic<0>{});
-  if (PF < n_stages) load_stage(ic<0>{}, PF);
+#pragma unroll
+  for (int i = 0; i < kPiecesPerWave; ++i)
+    if (piece_there(i) && !piece_is_v(i)) store_piece(i, first_k[i], 0);
+  store_step(ic<0>{}, ic<0>{});
+  load_step(ic<0>{}, PF);
   __syncthreads();
-  for (int t0 = 0; t0 < n_stages; t0 += PF) {
-    static_for<0, PF>([&](auto u_c) {
-      constexpr int u = decltype(u_c)::value;
-      const int t = t0 + u;
-      if (t < n_stages) {
-        if (t + 1 < n_stages) store_stage(ic<(u + 1) % PF>{}, ic<(u + 1) % 2>{});
-        if (t + 1 + PF < n_stages) load_stage(ic<(u + 1) % PF>{}, t + 1 + PF);
-        const int j = t * KG + kg;
-        if (j < n_tiles && wave_live) compute(j, ic<u % 2>{});
-        __syncthreads();
+  if (kg < n_tiles && wave_live) {
+    logits(s, ic<0>{});
+    sk = scale_of(k_scale, kg), sv = scale_of(v_scale, kg);
+  }
+  __syncthreads();
+  // Step t of the registers' ring: LDS has V of stage t and K of stage t + 1; what comes next goes where V of t - 1 and K of t were.
+  // (Loads behind the last stage repeat the prefix's last row: no branch, and a few bytes from a cache.)
+  int t = 0;
+  auto step = [&](auto u_c) __attribute__((always_inline)) {
+    constexpr int u = decltype(u_c)::value;
+    store_step(ic<(u + 1) % PF>{}, ic<(u + 1) % 2>{});
+    load_step(ic<(u + 1) % PF>{}, t + 1 + PF);
+    const int j = t * KG + kg;
+    if (__builtin_expect(wave_live && j < n_tiles, 1)) tile(j, ic<u % 2>{});
+    __syncthreads();
+    ++t;
+  };
+  // (Whole turns of the ring, then the rest: a loop that is left in its middle has paths that meet, and there the compiler waits for
+  // every load in flight.)
+  static_assert(PF == 2 || PF == 4, "the rest is written out");
+  for (int turns = n_stages / PF; turns > 0; --turns) static_for<0, PF>(step);
+  const int rest = n_stages % PF;
+  if (rest > 0) {
+    step(ic<0>{});
+    if constexpr (PF == 4) {
+      if (rest > 1) {
+        step(ic<1>{});
+        if (rest > 2) step(ic<2>{});
       }
-    });
+    }
   }
 
   run_sum = halves_sum(run_sum);
   const int64_t slot = static_cast<int64_t>(split) * p.Hq * p.T + g * M + row0 + c32;
-  if constexpr (KG == 1) {
+  if constexpr (KG == 1 && D == 128) {
+    // ---- fp16 against the row's largest element: the triple (reference, sum, O) is rescaled by the power of two that brings that just
+    // below 1, and goes through the wave's own part of LDS, so that whole rows are stored
+    float row_max = 0.f;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) row_max = fmaxf(row_max, fmaxf(fabsf(acc_o[db][r]), fabsf(acc_o[db][r + 1])));
+    row_max = halves_max(row_max);
+    const int row_exp = (row_max > 0.f && row_max < INFINITY) ? __builtin_amdgcn_frexp_expf(row_max) : 0;
+    const float row_scale = __builtin_amdgcn_ldexpf(1.0f, -row_exp);
+    unsigned char* priv = lds + wave * kPatchBytes;
+#pragma unroll
+    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        uintx2 w;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const floatx2 f = {acc_o[db][4 * r4 + 2 * e] * row_scale, acc_o[db][4 * r4 + 2 * e + 1] * row_scale};
+          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, halfx2));
+        }
+        *reinterpret_cast<uintx2*>(priv + c32 * kPatchStride + (32 * db + 8 * r4 + 4 * hf) * 2) = w;
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    uint16_t* part_h = reinterpret_cast<uint16_t*>(p.part_o) + (slot - c32) * D;
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+      const int row = 4 * it + (lane >> 4);
+      const uintx2* src = reinterpret_cast<const uintx2*>(priv + row * kPatchStride + 16 * (lane & 15));
+      const uintx2 a = src[0], b = src[1];
+      if (row0 + row < M) __builtin_nontemporal_store(uintx4{a[0], a[1], b[0], b[1]}, reinterpret_cast<uintx4*>(part_h + row * D + 8 * (lane & 15)));
+    }
+    if (hf == 0 && row0 + c32 < M)
+      __builtin_nontemporal_store(floatx2{ref + static_cast<float>(row_exp), run_sum * row_scale}, reinterpret_cast<floatx2*>(p.part_ml + slot * 2));
+  } else if constexpr (KG == 1) {
     if (row0 + c32 < M) {
       float* dst = p.part_o + slot * D;
 #pragma unroll
@@ -299,7 +380,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     }
     __syncthreads();
     float weight[KG];
-    float top = -INFINITY, total = 0.f;
+    float total = 0.f, top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < KG; ++w) top = fmaxf(top, ml[(w * R + r_block) * 64 + c32]);
 #pragma unroll
