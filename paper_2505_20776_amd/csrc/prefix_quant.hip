@@ -93,9 +93,17 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   auto piece_is_v = [&](int i) { return i * R + r_block >= kPieces / 2; };
   auto piece_row = [&](int i) { return (i * R + r_block) % (kPieces / 2) * kPieceRows + lane / kLanesPerRow; };
   auto piece_there = [&](int i) { return kPieces >= R || i * R + r_block < kPieces; };
-  auto load_piece = [&](int i, int stage) {
-    const int key = min(key_lo + (stage * KG + kg) * kTile + piece_row(i), L - 1);
-    return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>((piece_is_v(i) ? vbase : kbase) + key * kp_sl + (lane % kLanesPerRow) * 16));
+  // (offsets within a tile are 32 bits, from a uniform base: no 64-bit products on the vector ALUs)
+  const unsigned row_stride = static_cast<unsigned>(kp_sl);
+  unsigned in_tile[kPiecesPerWave];
+#pragma unroll
+  for (int i = 0; i < kPiecesPerWave; ++i) in_tile[i] = piece_row(i) * row_stride + (lane % kLanesPerRow) * 16;
+  auto load_piece = [&](int i, int stage) __attribute__((always_inline)) {
+    const int key0 = min(key_lo + (stage * KG + kg) * kTile, L - 1);
+    const unsigned char* at = (piece_is_v(i) ? vbase : kbase) + key0 * kp_sl;
+    unsigned off = in_tile[i];
+    if (__builtin_expect(key0 + kTile > L, 0)) off = min(piece_row(i), L - 1 - key0) * row_stride + (lane % kLanesPerRow) * 16;
+    return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(at + off));
   };
   // ---- LDS: per key group two K and two V tiles of 32 rows.  The 16-byte chunks of a row are XOR-swizzled so that the operand
   // reads are free of bank conflicts.
@@ -176,6 +184,12 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
       v_addr[db] = lds0 + kTileBytes + row * kRowBytes + (((4 * db + 2 * half16 + ((li & 3) >> 1)) ^ v_swizzle(row)) << 4) + ((li & 1) << 3);
   }
 
+  // in registers as they are, instead of an addition per use
+#pragma unroll
+  for (int ks = 0; ks < kSteps; ++ks) asm volatile("" : "+v"(k_addr[ks]));
+#pragma unroll
+  for (int db = 0; db < kBlocks; ++db) asm volatile("" : "+v"(v_addr[db]));
+
   const const_float* k_scale = (const const_float*)k_scale_at + g * scale_sh;
   const const_float* v_scale = (const const_float*)v_scale_at + g * scale_sh;
 
@@ -194,21 +208,42 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   // the tile whose softmax comes next
   floatx16 s = {};
   float sk = 0.f, sv = 0.f;      // and its scales
-  auto logits = [&](floatx16& x, auto buf_c) __attribute__((always_inline)) {
+  halfx8 kf[kSteps];
+  auto read_k = [&](auto buf_c) __attribute__((always_inline)) {
     constexpr int buf = decltype(buf_c)::value * 2 * kTileBytes;
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks)
+      kf[ks] = __builtin_bit_cast(halfx8, *reinterpret_cast<const lds_uintx4*>(static_cast<uintptr_t>(k_addr[ks] + buf)));
+  };
+  auto logits = [&](floatx16& x) __attribute__((always_inline)) {
     x = floatx16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) {
-      const uintx4 kw = *reinterpret_cast<const lds_uintx4*>(static_cast<uintptr_t>(k_addr[ks] + buf));
-      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, kw), qf[ks], x, 0, 0, 0);
-    }
+    for (int ks = 0; ks < kSteps; ++ks) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[ks], qf[ks], x, 0, 0, 0);
   };
   auto scale_of = [&](const const_float* scale, int j) { return scale[min(key_lo + j * kTile, key_hi - 1) >> block_log2]; };
   // Tile j from its logits in s on, and the logits of tile j + KG into the matrix pipe while the vector ALUs take the exponentials.
   // (Behind the last tile those are of whatever the buffer holds, and nobody reads them: cheaper than a second form of the loop's
   // body, whose registers would spill.)
+  halfx8 p0 = {}, p1 = {};       // probabilities of the tile whose second product comes next
+  halfx8 vf[2][kBlocks] = {};
+  auto read_v = [&](auto buf_c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db) {
+        const unsigned at = v_addr[db] + decltype(buf_c)::value * 2 * kTileBytes + 16 * jj * kRowBytes;
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at + 8 * kRowBytes));
+        vf[jj][db] = __builtin_bit_cast(halfx8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+  };
+  auto second_product = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int db = 0; db < kBlocks; ++db) acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[jj][db], jj ? p1 : p0, acc_o[db], 0, 0, 0);
+  };
   auto tile = [&](int j, auto buf_c) __attribute__((always_inline)) {
-    constexpr int buf = decltype(buf_c)::value;
     const int key0 = key_lo + j * kTile;
     // register r holds key key0 + 8 (r / 4) + 4 hf + r % 4
     if (__builtin_expect(key0 + kTile > key_hi, 0)) {
@@ -235,8 +270,9 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
         for (int r = 0; r < 16; ++r) acc_o[db][r] *= alpha;
     }
     sk = scale_of(k_scale, j + KG), sv = scale_of(v_scale, j + KG);
+    read_v(buf_c);
     floatx16 next;
-    logits(next, ic<1 - buf>{});
+    logits(next);
     const float shift = lsv - ref;
     float part = 0.f;
 #pragma unroll
@@ -249,8 +285,8 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     asm volatile("" : "+v"(run_sum));        // here, not behind the next branch
     // every lane stores: the two lanes of a row hold the same pair, and so do padding rows
     if (SCORES) *reinterpret_cast<floatx2*>(score_base + j * score_step + score_off) = floatx2{halves_sum(part), ref};
-    const halfx8 p0 = pack8_f16(s, 0), p1 = pack8_f16(s, 8);
-    __builtin_amdgcn_sched_group_barrier(0x100, kSteps, 0);         // LDS reads
+    p0 = pack8_f16(s, 0), p1 = pack8_f16(s, 8);
+    __builtin_amdgcn_sched_group_barrier(0x100, 4 * kBlocks, 0);    // LDS reads
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {                              // a matrix instruction, then its share of the exponentials
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -261,19 +297,6 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     // first reader allows for, and that reader (two logits of a lane) now and then saw the sum of seven eighths of the row.
     asm volatile("" : "+v"(next));
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db) {
-      halfx8 vf[2];
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        const unsigned at = v_addr[db] + buf * 2 * kTileBytes + 16 * jj * kRowBytes;
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at));
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)static_cast<uintptr_t>(at + 8 * kRowBytes));
-        vf[jj] = __builtin_bit_cast(halfx8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[0], p0, acc_o[db], 0, 0, 0);
-      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[1], p1, acc_o[db], 0, 0, 0);
-    }
     s = next;
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -285,19 +308,27 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   load_step(ic<0>{}, PF);
   __syncthreads();
   if (kg < n_tiles && wave_live) {
-    logits(s, ic<0>{});
+    read_k(ic<0>{});
+    logits(s);
     sk = scale_of(k_scale, kg), sv = scale_of(v_scale, kg);
   }
   __syncthreads();
   // Step t of the registers' ring: LDS has V of stage t and K of stage t + 1; what comes next goes where V of t - 1 and K of t were.
   // (Loads behind the last stage repeat the prefix's last row: no branch, and a few bytes from a cache.)
+  // Behind a barrier all waves want K from LDS at once, 64 KB for eight of them and 512 cycles; so a tile's second product, its
+  // operands in registers, waits for the other side of the barrier and fills the matrix pipe meanwhile, as the next logits do while V
+  // comes.
   int t = 0;
   auto step = [&](auto u_c) __attribute__((always_inline)) {
     constexpr int u = decltype(u_c)::value;
+    read_k(ic<1 - u % 2>{});
+    __builtin_amdgcn_sched_barrier(0);
+    second_product();
     store_step(ic<(u + 1) % PF>{}, ic<(u + 1) % 2>{});
     load_step(ic<(u + 1) % PF>{}, t + 1 + PF);
     const int j = t * KG + kg;
     if (__builtin_expect(wave_live && j < n_tiles, 1)) tile(j, ic<u % 2>{});
+    else p0 = p1 = halfx8{};
     __syncthreads();
     ++t;
   };
@@ -315,6 +346,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
       }
     }
   }
+  second_product();
 
   run_sum = halves_sum(run_sum);
   const int64_t slot = static_cast<int64_t>(split) * p.Hq * p.T + g * M + row0 + c32;
