@@ -18,9 +18,10 @@ EXTRA_FLAGS = {"prefix_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "prefix_mfma_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
                "prefix_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
                "prefill_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
-               "prefix_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
+               "prefix_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+               "prefix_quant_few.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
 SOURCES = ["api.hip", "prefix_generic.hip", "prefix_mfma.hip", "prefix_mfma_rows.hip", "prefix_f32.hip", "tree_merge.hip", "retrieval.hip",
-           "accept.hip", "materialized.hip", "prefill_rows.hip", "calibrate.hip", "api_quant.hip", "prefix_quant.hip", "quant_cache.hip",
+           "accept.hip", "materialized.hip", "prefill_rows.hip", "calibrate.hip", "api_quant.hip", "prefix_quant.hip", "prefix_quant_few.hip", "quant_cache.hip",
            "token_logprobs.hip"]
 
 

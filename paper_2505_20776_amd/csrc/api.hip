@@ -193,7 +193,7 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   // x 2) 28.8 / 28.4, 800 (8 x 1.75 / 7 x 2) 30.6 / 29.5, 1300 (8 x 2.75 / 7 x 3) 34.3 / 33.3, bf16 1200 (8 x 1.25 / 5 x 2) 22.6 / 21.8.
   // A requested count is always cut at tiles, so that the one that an automatic call reports gives as many splits again; only
   // where the static scratch array cannot hold a requested count is that cut at stages, which makes fewer splits.
-  int64_t unit = p->use_mfma == 1 ? 128 : 64;
+  int64_t unit = p->use_mfma == 1 || (p->use_mfma == 4 && p->rows_per_group <= 64) ? 128 : 64;
   const int stage = p->in_dtype == SPECEXT_BF16 ? 128 : 64;
   if (p->use_mfma == 3) unit = stage_cut && d->num_splits != 0 ? stage : stage / 4;
   if (p->want_scores && p->use_mfma != 3) unit = unit / gcd64(unit, p->B) * p->B;

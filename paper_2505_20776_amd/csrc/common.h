@@ -117,6 +117,7 @@ hipError_t launch_prefix_f32(const AttnParams& p, hipStream_t stream);         /
 hipError_t launch_prefix_mfma(const AttnParams& p, hipStream_t stream);        // key-split kernel (use_mfma == 1)
 hipError_t launch_prefix_mfma_rows(const AttnParams& p, hipStream_t stream);   // row-split kernel (use_mfma == 2)
 hipError_t launch_prefix_quant(const AttnParams& p, const QuantScales& scales, hipStream_t stream);   // 8-bit prefix (use_mfma == 4)
+hipError_t launch_prefix_quant_few(const AttnParams& p, const QuantScales& scales, hipStream_t stream);   // the same, up to 64 rows per KV head
 hipError_t launch_tree_merge(const AttnParams& p, hipStream_t stream);
 // score_row >= 0: that row; -1: every row; row_path != nullptr: the row is read on the device,
 // row_path[*row_count - 1] (row 0 when *row_count <= 0)

@@ -462,18 +462,14 @@ hipError_t launch_one(const AttnParams& p, const QuantScales& s, hipStream_t str
 
 template <int D, bool SCORES>
 hipError_t launch_rows(const AttnParams& p, const QuantScales& s, hipStream_t stream) {
-  switch (p.rows_per_group) {
-    case 32: return launch_one<D, 1, 4, 2, SCORES>(p, s, stream);
-    case 64: return launch_one<D, 2, 4, 2, SCORES>(p, s, stream);
-    case 128: return launch_one<D, 4, 2, 2, SCORES>(p, s, stream);
-    default: return launch_one<D, 8, 1, 4, SCORES>(p, s, stream);
-  }
+  return p.rows_per_group == 128 ? launch_one<D, 4, 2, 2, SCORES>(p, s, stream) : launch_one<D, 8, 1, 4, SCORES>(p, s, stream);
 }
 
 }  // namespace
 
 hipError_t launch_prefix_quant(const AttnParams& p, const QuantScales& s, hipStream_t stream) {
   if (p.S <= 0) return hipSuccess;
+  if (p.rows_per_group <= 64) return launch_prefix_quant_few(p, s, stream);
   if (p.d == 128) return p.want_scores ? launch_rows<128, true>(p, s, stream) : launch_rows<128, false>(p, s, stream);
   return p.want_scores ? launch_rows<64, true>(p, s, stream) : launch_rows<64, false>(p, s, stream);
 }
