@@ -82,8 +82,8 @@ typedef enum specext_dtype {
  * 32, 64 or 128 tokens of a KV head; each flag's value is its number of tokens.  Such a descriptor belongs to
  * specext_verify_attn_quant; specext_workspace_bytes, specext_num_splits and the chunk-score functions take it too, the
  * other attention functions refuse it (SPECEXT_ERR_INVALID_ARG).  dtype has to be SPECEXT_BF16 (queries and tree),
- * chunk_size a multiple of 32 when want_scores is set, kp_stride_* multiples of 16, and SPECEXT_FLAG_VALU_PREFIX unset
- * (SPECEXT_ERR_UNSUPPORTED otherwise); SPECEXT_FLAG_FUSED_MERGE has no effect. */
+ * chunk_size a multiple of 32 when want_scores is set, kp_stride_* multiples of 16, kp_stride_l at most 2^24, the queries
+ * within 2^30 elements, and SPECEXT_FLAG_VALU_PREFIX unset (SPECEXT_ERR_UNSUPPORTED otherwise); SPECEXT_FLAG_FUSED_MERGE has no effect. */
 #define SPECEXT_FLAG_QUANT_BLOCK_32 32u
 #define SPECEXT_FLAG_QUANT_BLOCK_64 64u
 #define SPECEXT_FLAG_QUANT_BLOCK_128 128u
@@ -497,8 +497,8 @@ int specext_commit_tree_quant(const void* k_tree, const void* v_tree, void* k_ca
  * [Hkv, L, d] (kp_stride_* in bytes), k_scale / v_scale fp32 [Hkv, ceil(L / block)] with scale_stride_h floats from head
  * to head (0: ceil(L / block)).  Queries, tree and everything else as there; n_tree = 1 is the decoding of one token.
  * Logits are exact products of the e4m3 keys and the bf16 queries summed in fp32 (query elements below 2^-22 of their
- * row's largest lose bits); probabilities enter the matrix cores as fp16, split partials cross memory as fp32, or as
- * fp16 after a per-row power-of-two rescale with head_dim 128 and more than 128 rows per KV head.
+ * row's largest lose bits); probabilities enter the matrix cores as fp16, split partials cross memory as fp32, or with
+ * head_dim 128 as fp16 after a per-row power-of-two rescale.
  * specext_chunk_scores and its kin read the same workspace with the same desc.
  */
 int specext_verify_attn_quant(const specext_desc* desc, const void* q, const void* k_prefix, const void* v_prefix, const float* k_scale,

@@ -103,9 +103,10 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   for (int64_t s : strides)
     if (s < 0 || s % 8 != 0) return SPECEXT_ERR_UNSUPPORTED;
   if (p->q_sh < p->d || p->kp_sl < p->d || p->kt_st < p->d || p->o_sh < p->d) return SPECEXT_ERR_INVALID_ARG;
-  // a prefix in 8 bits: one kernel, rows of 16-byte pieces
+  // a prefix in 8 bits: rows of 16-byte pieces, 32-bit offsets within a tile and within the queries
   if (quant_block && (d->dtype != SPECEXT_BF16 || (p->want_scores && p->B % 32 != 0) || (d->flags & SPECEXT_FLAG_VALU_PREFIX) ||
-                      p->kp_sh % 16 != 0 || p->kp_sl % 16 != 0))
+                      p->kp_sh % 16 != 0 || p->kp_sl % 16 != 0 || p->kp_sl > (1 << 24) ||
+                      (p->T - 1) * p->q_st + (p->Hq - 1) * p->q_sh + p->d >= (int64_t{1} << 30)))
     return SPECEXT_ERR_UNSUPPORTED;
 
   // Which prefix kernel runs.  The matrix-core kernels take bf16, d = 128, at least one
@@ -132,7 +133,7 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   if (quant_block) {
     p->use_mfma = 4;
     p->rows_per_group = p->M <= 32 ? 32 : p->M <= 64 ? 64 : p->M <= 128 ? 128 : 256;
-    p->part_f16 = p->d == 128 && p->rows_per_group == 256;
+    p->part_f16 = p->d == 128;
   } else if (mfma64_ok) {
     p->use_mfma = 2;
     p->rows_per_group = p->M > 128 ? 256 : 128;

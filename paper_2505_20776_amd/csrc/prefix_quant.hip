@@ -17,7 +17,7 @@
 // workgroup and stores them to one of two LDS buffers, while the waves compute on the other: one barrier per stage of KG tiles.
 // From there on the tile is that of the bf16 kernels: S^T = K Q^T and O^T += V^T P^T with a lane owning one query row in both
 // products, V through the transposing LDS read, P straight from the accumulator registers.
-#include "mfma_util.h"
+#include "quant_merge.h"
 
 namespace specext {
 namespace {
@@ -34,7 +34,7 @@ constexpr int kPatchBytes = 32 * kPatchStride;
 template <int D, int R, int KG>
 constexpr int lds_bytes() {
   const int buffers = 2 * KG * 2 * tile_bytes<D>();
-  const int end = KG > 1 ? R * KG * (D * kTile * 4 + 2 * 32 * 4) : D == 128 ? R * kPatchBytes : 0;
+  const int end = KG > 1 ? merge_bytes<D>(R * KG) : D == 128 ? R * kPatchBytes : 0;
   return buffers > end ? buffers : end;
 }
 
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
   float c;
   {
     const int m = min(row0 + c32, M - 1);        // padding rows repeat the last real row (never stored)
-    const int t = m / G;
+    const int t = static_cast<int>((static_cast<float>(m) + 0.5f) * (1.0f / static_cast<float>(G)));     // m / G, exact for m < 2^20
     const int h = g * G + (m - t * G);
     const unsigned char* src = in_global<const unsigned char>(q_at) + (t * p.q_st + h * p.q_sh + 8 * hf) * 2;
     uintx4 w[kSteps];
@@ -398,43 +398,11 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
       if (hf == 0) __builtin_nontemporal_store(floatx2{ref, run_sum}, reinterpret_cast<floatx2*>(p.part_ml + slot * 2));
     }
   } else {
-    // ---- the key groups' partials of a row block meet in LDS; each group finishes its share of the registers
-    constexpr int kRegs = kBlocks * 16;
+    // ---- the key groups' partials of a row block meet in LDS
     float* dump = reinterpret_cast<float*>(lds);
-    float* ml = dump + R * KG * kRegs * 64;      // [wave][2][32]
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dump[(wave * kRegs + db * 16 + r) * 64 + lane] = acc_o[db][r];
-    if (hf == 0) {
-      ml[wave * 64 + c32] = ref;
-      ml[wave * 64 + 32 + c32] = run_sum;
-    }
+    dump_wave<D>(dump, R * KG, wave, acc_o, ref, run_sum, lane);
     __syncthreads();
-    float weight[KG];
-    float total = 0.f, top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < KG; ++w) top = fmaxf(top, ml[(w * R + r_block) * 64 + c32]);
-#pragma unroll
-    for (int w = 0; w < KG; ++w) {
-      const float sum = ml[(w * R + r_block) * 64 + 32 + c32];
-      weight[w] = sum > 0.f ? fast_exp2(ml[(w * R + r_block) * 64 + c32] - top) : 0.f;     // a group without tiles: nothing
-      total = fmaf(sum, weight[w], total);
-    }
-    if (row0 + c32 < M) {
-      float* dst = p.part_o + slot * D;
-#pragma unroll
-      for (int i = 0; i < kRegs / KG; i += 4) {
-        const int first = kg * (kRegs / KG) + i;
-        floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < KG; ++w)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = fmaf(dump[((w * R + r_block) * kRegs + first + e) * 64 + lane], weight[w], o[e]);
-        __builtin_nontemporal_store(o, reinterpret_cast<floatx4*>(dst + 32 * (first >> 4) + 2 * (first & 15) + 4 * hf));
-      }
-      if (kg == 0 && hf == 0) __builtin_nontemporal_store(floatx2{top, total}, reinterpret_cast<floatx2*>(p.part_ml + slot * 2));
-    }
+    merge_groups<D, KG>(dump, R * KG, r_block, R, kg, M - row0, p.part_o, p.part_ml, slot - c32, lane);
   }
 }
 

@@ -7,7 +7,7 @@
 // bytes, each widened to fp16 in registers, once.  The order of a row's elements within the contraction is the one that the 16-byte
 // pieces give, for keys and queries alike; the order of the keys is that of the logits in their accumulator.
 //
-#include "mfma_util.h"
+#include "quant_merge.h"
 
 namespace specext {
 namespace {
@@ -26,7 +26,7 @@ __host__ __device__ constexpr int slot_bytes() { return 2 * kTile * D; }        
 template <int D, int RB>
 constexpr int lds_bytes() {
   const int ring = kWaves * kSlots * slot_bytes<D>();
-  const int merge = kWaves * RB * (D * kTile * 4 + 2 * 32 * 4);
+  const int merge = merge_bytes<D>(kWaves * RB);
   return ring > merge ? ring : merge;
 }
 
@@ -135,16 +135,18 @@ __global__ __launch_bounds__(kWaves * 64) void prefix_quant_few_kernel(uint64_t 
   auto q_swizzle = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   const unsigned q_lds = ring_lds + (kSlots - kQSlots) * slot_bytes<D>();
   if (n > 0) {
+    const float inv_g = 1.0f / static_cast<float>(G);
+    const unsigned q_st = static_cast<unsigned>(p.q_st) * 2u, q_sh = static_cast<unsigned>(p.q_sh) * 2u;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int u = 0; u < kQLoads; ++u) {
         const int row = u * kQLoadRows + lane / kQChunks;
         const int m = min(32 * rb + row, M - 1);             // padding rows repeat the last real row (never stored)
-        const int t = m / G;
+        const int t = static_cast<int>((static_cast<float>(m) + 0.5f) * inv_g);       // m / G, exact for m < 2^20
         const int h = g * G + (m - t * G);
-        load_to_lds_16_at(q_lds + (rb * kQLoads + u) * 1024, in_global<const unsigned char>(q_at) + (t * p.q_st + h * p.q_sh) * 2 +
-                                                                 (((lane % kQChunks) ^ q_swizzle(row)) << 4));
+        load_to_lds_16(q_lds + (rb * kQLoads + u) * 1024, t * q_st + h * q_sh + (((lane % kQChunks) ^ q_swizzle(row)) << 4),
+                       in_global<const unsigned char>(q_at));
       }
 #pragma unroll
     for (int j = 0; j < kSlots - kQSlots; ++j)
@@ -320,54 +322,18 @@ __global__ __launch_bounds__(kWaves * 64) void prefix_quant_few_kernel(uint64_t 
     }
   }
 
-  // ---- the four waves' partials meet in LDS; each finishes a quarter of the registers
-  constexpr int kRegs = kBlocks * 16;
+  // ---- the four waves' partials of a block of rows meet in LDS
   float* dump = reinterpret_cast<float*>(lds);
-  float* ml = dump + kWaves * RB * kRegs * 64;       // [wave][rb][2][32]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) run_sum[rb] = halves_sum(run_sum[rb]);
   __syncthreads();                                   // every wave is done with its ring
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dump[((wave * RB + rb) * kRegs + db * 16 + r) * 64 + lane] = acc_o[rb][db][r];
-    if (hf == 0) {
-      ml[(wave * RB + rb) * 64 + c32] = ref[rb];
-      ml[(wave * RB + rb) * 64 + 32 + c32] = run_sum[rb];
-    }
-  }
+  for (int rb = 0; rb < RB; ++rb) dump_wave<D>(dump, kWaves * RB, wave * RB + rb, acc_o[rb], ref[rb], run_sum[rb], lane);
   __syncthreads();
+  const int64_t slot0 = static_cast<int64_t>(split) * p.Hq * p.T + g * M;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    float weight[kWaves];
-    float total = 0.f, top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[(w * RB + rb) * 64 + c32]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float sum = ml[(w * RB + rb) * 64 + 32 + c32];
-      weight[w] = sum > 0.f ? fast_exp2(ml[(w * RB + rb) * 64 + c32] - top) : 0.f;       // a wave without tiles: nothing
-      total = fmaf(sum, weight[w], total);
-    }
-    const int m = 32 * rb + c32;
-    if (m < M) {
-      const int64_t slot = static_cast<int64_t>(split) * p.Hq * p.T + g * M + m;
-      float* dst = p.part_o + slot * D;
-#pragma unroll
-      for (int i = 0; i < kRegs / kWaves; i += 4) {
-        const int first = wave * (kRegs / kWaves) + i;
-        floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = fmaf(dump[((w * RB + rb) * kRegs + first + e) * 64 + lane], weight[w], o[e]);
-        __builtin_nontemporal_store(o, reinterpret_cast<floatx4*>(dst + 32 * (first >> 4) + 2 * (first & 15) + 4 * hf));
-      }
-      if (wave == 0 && hf == 0) __builtin_nontemporal_store(floatx2{top, total}, reinterpret_cast<floatx2*>(p.part_ml + slot * 2));
-    }
-  }
+  for (int rb = 0; rb < RB; ++rb)
+    merge_groups<D, kWaves>(dump, kWaves * RB, rb, RB, wave, M - 32 * rb, p.part_o, p.part_ml, slot0 + 32 * rb, lane);
 }
 
 template <int D, int RB, bool SCORES>
