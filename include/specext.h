@@ -134,7 +134,7 @@ const char* specext_strerror(int status);
  * descriptor: a shorter prefix may be cut into more splits.  With bf16 inputs, an automatic
  * split count and chunks of whole 32 keys (or no scores) the size covers that up to prefixes of
  * 1024 keys, so that one workspace serves shorter prefixes and smaller trees as well as splits
- * of 128 keys would let it.
+ * of 128 keys would let it (not so with an 8-bit prefix, whose descriptors are asked for one by one).
  * Host-only; needs a visible GPU only when num_splits == 0 (to read the
  * compute-unit count).
  */

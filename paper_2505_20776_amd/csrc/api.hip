@@ -178,7 +178,20 @@ int resolve(const specext_desc* d, AttnParams* p, bool stage_cut = false, bool n
   const int groups_128 = (p->M + 127) / 128;
   const int64_t workgroups_64 = static_cast<int64_t>(at_most_16(64)) * p->Hkv * groups_128;
   const bool by_64 = !no_64 && p->use_mfma == 2 && (p->d == 64 && groups_128 > 1 ? workgroups_64 * 2 <= device_cu_count() : workgroups_64 * 3 <= device_cu_count() * 2);
-  const int by_256 = static_cast<int>((p->L + 255) / 256), by_less = at_most_16(by_64 ? 64 : 128);
+  const int by_256 = static_cast<int>((p->L + 255) / 256);
+  int by_less = at_most_16(by_64 ? 64 : 128);
+  if (quant_block) {
+    // 8-bit prefix: half the bytes per split, so shorter ones: 128 keys up to 32 splits where those are at most 128 rows, or fill no
+    // more than half of the device; 64 keys for a prefix of at most 512 under more than 64 rows, whose work per key is the larger.
+    // Attention call in a graph, us, 32 heads in 8 groups unless noted: 4096 keys in 16 / 32 splits, 1 node 9.65 / 9.0, 16 nodes 15.0 /
+    // 13.7, 30 nodes 16.7 / 16.2, 60 nodes 18.35 / 18.5, 60 nodes of 8 heads in 2 groups 16.5 / 14.4, 60 nodes 64-wide 15.7 / 16.8; 60
+    // nodes 512 keys in 4 / 8 14.0 / 13.4, 256 in 2 / 4 13.7 / 12.7, but 1024 in 8 / 16 14.55 / 14.9.
+    const int64_t groups = static_cast<int64_t>(p->Hkv) * ((p->M + p->rows_per_group - 1) / p->rows_per_group);
+    const int keys = p->M > 64 && p->L <= 512 ? 64 : 128;
+    const int most = p->M <= 128 || groups * 32 * 2 <= device_cu_count() ? 32 : 16;
+    by_less = static_cast<int>((p->L + keys - 1) / keys);
+    if (by_less > most) by_less = most;
+  }
   const int by_len = by_256 > by_less ? by_256 : by_less;
   // With so few splits that workgroups of 128 rows still fit the device at once, the row-split kernel takes those: twice as
   // many compute units, and a wave has its SIMD to itself.  Every K/V byte then enters two compute units, of one XCD where

@@ -132,3 +132,28 @@ def test_logits(sx):
                        (dict(logits=OK + 1), -2), (dict(logits=OK + 2, dtype=0), -2), (dict(ws=OK + 128), -2), (dict(lse=OK + 2), -2),
                        (dict(entropy=OK + 1), -2), (dict(top_id=OK + 2), -2), (dict(tokens=OK + 2), -2), (dict(workspace_nbytes=nbytes - 1), -3)]:
         assert call(**kw) == status, kw
+
+
+@pytest.mark.parametrize("d,hq,hkv,T,L,splits", [
+    (128, 32, 8, 1, 2048, 16), (128, 32, 8, 1, 4096, 32), (128, 32, 8, 16, 4096, 32), (128, 32, 8, 30, 4096, 32), (128, 32, 8, 60, 4096, 16),
+    (128, 8, 2, 60, 4096, 32), (128, 32, 8, 60, 512, 8), (128, 32, 8, 60, 513, 5), (128, 32, 8, 8, 512, 4), (64, 12, 12, 60, 4096, 16),
+    (128, 32, 8, 128, 32731, 16), (128, 32, 32, 60, 8155, 8), (128, 32, 8, 1, 1, 1)])
+def test_automatic_splits(sx, d, hq, hkv, T, L, splits):
+    """256 compute units: 128 keys up to 32 splits for at most 128 rows per KV head or few KV heads, else 16; 64 keys up to 512."""
+    for block in (32, 64, 128):
+        for chunk in (0, 32):
+            kw = dict(dtype=sx.SPECEXT_BF16, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, prefix_len=L, n_tree=T, flags=block, chunk_size=chunk,
+                      want_scores=chunk > 0)
+            assert sx.num_splits(sx.make_desc(**kw)) == splits
+            assert sx.num_splits(sx.make_desc(num_splits=splits, **kw)) == splits
+
+
+@pytest.mark.parametrize("d,hq,hkv,T", [(128, 32, 8, 1), (128, 32, 8, 16), (128, 32, 8, 30), (128, 32, 8, 60), (128, 8, 2, 128), (64, 12, 12, 60), (64, 32, 8, 60)])
+def test_the_reported_split_count_holds_at_every_length(sx, d, hq, hkv, T):
+    for L in [*range(1, 1200, 7), *range(1200, 8300, 97), 16384, 50000, 131035]:
+        for chunk in (0, 32, 96, 1024):
+            kw = dict(dtype=sx.SPECEXT_BF16, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, prefix_len=L, n_tree=T, chunk_size=chunk, want_scores=chunk > 0,
+                      flags=64)
+            auto = sx.make_desc(**kw)
+            asked = sx.make_desc(num_splits=sx.num_splits(auto), **kw)
+            assert sx.num_splits(asked) == sx.num_splits(auto) and sx.workspace_bytes(asked) == sx.workspace_bytes(auto), (L, chunk)
