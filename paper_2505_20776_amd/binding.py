@@ -6,7 +6,7 @@ passes their data pointers and the current HIP stream and checks the returned
 status.  No arithmetic of the method happens in Python.  If the shared library
 is missing, loading raises: there is no fallback path.
 
-The functions that a decoding step calls are taken over, for plain arguments, by
+The functions that a decoding step calls, and those of the 8-bit cache and of the logits, are taken over, for plain arguments, by
 callables of the same signature that marshal natively (csrc/marshal.cpp; a call of
 ten tensors 1.9 -> 0.3 us); everything else comes back to the functions here.  They
 are copied, pickled, weakly referenced, given attributes and bound as functions are,
@@ -155,7 +155,7 @@ def load_library() -> ctypes.CDLL:
     _lib = lib
     _take_over()            # built since this module was imported
     if _marshal is not None:
-        for name in _marshal.FUNCTIONS:
+        for name in _marshal.FUNCTIONS + _marshal.QUANT_FUNCTIONS:
             _marshal.bind(name, ctypes.cast(getattr(lib, "specext_" + name), ctypes.c_void_p).value)
     elif _marshal_error is not None:
         warnings.warn(f"{_MARSHAL_PATH} {_marshal_error}: calls are marshalled through ctypes, 2 us more each, "
@@ -507,6 +507,7 @@ def _take_over() -> None:
     importlib.invalidate_caches()
     try:
         from . import _marshal as native
+        names = native.FUNCTIONS + native.QUANT_FUNCTIONS       # (an older build has no second list: not this package's)
     except Exception as e:
         _marshal_error = f"does not load ({type(e).__name__}: {e})"
         return
@@ -514,7 +515,7 @@ def _take_over() -> None:
     if _raw_stream is not None:
         native.set_stream_ready()
     package = sys.modules[__package__]
-    for name in native.FUNCTIONS:
+    for name in names:
         plain = globals()[name]
         globals()[name] = native.wrap(name, plain, specext_desc, _check)
         if getattr(package, name, None) is plain:           # the package has imported its names by now

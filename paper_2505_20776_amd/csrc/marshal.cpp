@@ -57,7 +57,7 @@ Param opt_f(const char* n, float v) {
   return p;
 }
 
-constexpr int kMaxParams = 24;
+constexpr int kMaxParams = 32;
 
 // One function: its parameters in Python's order, and the call with the slots in that order.
 struct Function {
@@ -77,6 +77,13 @@ using L = int64_t;
 
 I i32(const Slot& s) { return static_cast<I>(s.i); }
 size_t bytes(const Slot& s) { return static_cast<size_t>(s.i); }
+
+// quant_kv_write and quant_kv_read: six pointers, eight numbers, eight strides
+int rows_call(void* fn, const Slot* s) {
+  return reinterpret_cast<int (*)(P, P, P, P, P, P, I, I, I, I, I, I, I, I, L, L, L, L, L, L, L, L, P)>(fn)(
+      s[0].p, s[1].p, s[2].p, s[3].p, s[4].p, s[5].p, i32(s[6]), i32(s[7]), i32(s[8]), i32(s[9]), i32(s[10]), i32(s[11]), i32(s[12]),
+      i32(s[13]), s[14].i, s[15].i, s[16].i, s[17].i, s[18].i, s[19].i, s[20].i, s[21].i, s[22].p);
+}
 
 Function functions[] = {
     {"verify_attn", 13,
@@ -163,7 +170,59 @@ Function functions[] = {
            s[0].p, s[1].p, s[2].p, s[3].p, s[4].p, i32(s[5]), i32(s[6]), i32(s[7]), i32(s[8]), i32(s[9]), i32(s[10]),
            i32(s[11]), s[12].f, s[13].i, s[14].i, s[15].i, s[16].i, s[17].i, s[18].i, s[19].p);
      }},
+    // ---- the functions of the 8-bit cache and of the logits, listed apart (kDecoding)
+    {"verify_attn_quant", 16,
+     {need("desc", kDesc), need("q", kPtr), need("k_prefix", kPtr), need("v_prefix", kPtr), need("k_scale", kPtr),
+      need("v_scale", kPtr), need("k_tree", kPtr), need("v_tree", kPtr), need("parent", kPtr), need("out", kPtr),
+      need("lse", kPtr), need("workspace", kPtr), opt("workspace_nbytes", kBytes), opt("scale_stride_h", kI64),
+      opt("stream", kStream), opt("check", kCheck, 1)},
+     [](void* fn, const Slot* s) {
+       return reinterpret_cast<int (*)(P, P, P, P, P, P, P, P, P, P, P, P, size_t, L, P)>(fn)(
+           s[0].p, s[1].p, s[2].p, s[3].p, s[4].p, s[5].p, s[6].p, s[7].p, s[8].p, s[9].p, s[10].p, s[11].p, bytes(s[12]), s[13].i,
+           s[14].p);
+     }},
+    {"quant_kv_write", 24,
+     {need("k_src", kPtr), need("v_src", kPtr), need("k_cache", kPtr), need("v_cache", kPtr), need("k_scale", kPtr),
+      need("v_scale", kPtr), need("n_layers", kI32), need("n_kv_heads", kI32), need("head_dim", kI32), need("n_tokens", kI32),
+      need("start", kI32), need("cache_capacity", kI32), need("scale_block", kI32), opt("dtype", kI32, 1),
+      opt("src_stride_layer", kI64), opt("src_stride_h", kI64), opt("src_stride_t", kI64), opt("cache_stride_layer", kI64),
+      opt("cache_stride_h", kI64), opt("cache_stride_l", kI64), opt("scale_stride_layer", kI64), opt("scale_stride_h", kI64),
+      opt("stream", kStream), opt("check", kCheck, 1)},
+     rows_call},
+    {"quant_kv_read", 24,
+     {need("k_cache", kPtr), need("v_cache", kPtr), need("k_scale", kPtr), need("v_scale", kPtr), need("k_dst", kPtr),
+      need("v_dst", kPtr), need("n_layers", kI32), need("n_kv_heads", kI32), need("head_dim", kI32), need("n_tokens", kI32),
+      need("start", kI32), need("cache_capacity", kI32), need("scale_block", kI32), opt("dtype", kI32, 1),
+      opt("dst_stride_layer", kI64), opt("dst_stride_h", kI64), opt("dst_stride_t", kI64), opt("cache_stride_layer", kI64),
+      opt("cache_stride_h", kI64), opt("cache_stride_l", kI64), opt("scale_stride_layer", kI64), opt("scale_stride_h", kI64),
+      opt("stream", kStream), opt("check", kCheck, 1)},
+     rows_call},
+    {"commit_tree_quant", 27,
+     {need("k_tree", kPtr), need("v_tree", kPtr), need("k_cache", kPtr), need("v_cache", kPtr), need("k_scale", kPtr),
+      need("v_scale", kPtr), need("path", kPtr), need("n_accept", kPtr), need("max_accept", kI32), need("n_tree", kI32),
+      need("n_layers", kI32), need("n_kv_heads", kI32), need("head_dim", kI32), need("prefix_len", kI32),
+      need("cache_capacity", kI32), need("scale_block", kI32), opt("dtype", kI32, 1), opt("tree_stride_layer", kI64),
+      opt("tree_stride_h", kI64), opt("tree_stride_t", kI64), opt("cache_stride_layer", kI64), opt("cache_stride_h", kI64),
+      opt("cache_stride_l", kI64), opt("scale_stride_layer", kI64), opt("scale_stride_h", kI64), opt("stream", kStream),
+      opt("check", kCheck, 1)},
+     [](void* fn, const Slot* s) {
+       return reinterpret_cast<int (*)(P, P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, I, L, L, L, L, L, L, L, L, P)>(fn)(
+           s[0].p, s[1].p, s[2].p, s[3].p, s[4].p, s[5].p, s[6].p, s[7].p, i32(s[8]), i32(s[9]), i32(s[10]), i32(s[11]), i32(s[12]),
+           i32(s[13]), i32(s[14]), i32(s[15]), i32(s[16]), s[17].i, s[18].i, s[19].i, s[20].i, s[21].i, s[22].i, s[23].i, s[24].i,
+           s[25].p);
+     }},
+    {"token_logprobs", 18,
+     {need("logits", kPtr), need("n_rows", kI32), need("vocab", kI32), need("workspace", kPtr), opt("dtype", kI32, 1),
+      opt("row_stride", kI64), opt_f("logit_scale", 0.f), opt("tokens", kPtr), opt("n_given", kI32), opt("logprob", kPtr),
+      opt("k", kI32), opt("top_id", kPtr), opt("top_logprob", kPtr), opt("lse", kPtr), opt("entropy", kPtr),
+      opt("workspace_nbytes", kBytes), opt("stream", kStream), opt("check", kCheck, 1)},
+     [](void* fn, const Slot* s) {
+       return reinterpret_cast<int (*)(P, I, I, I, L, float, P, I, P, I, P, P, P, P, P, size_t, P)>(fn)(
+           s[0].p, i32(s[4]), i32(s[1]), i32(s[2]), s[5].i, s[6].f, s[7].p, i32(s[8]), s[9].p, i32(s[10]), s[11].p, s[12].p, s[13].p,
+           s[14].p, s[3].p, bytes(s[15]), s[16].p);
+     }},
 };
+constexpr int kDecoding = 10;      // of these, the first: FUNCTIONS of the module; the others are QUANT_FUNCTIONS
 
 bool stream_ready = false;      // the GPU runtime is up (Python has read a current stream once)
 
@@ -428,10 +487,13 @@ PyMODINIT_FUNC PyInit__marshal() {
   if (PyType_Ready(&call_type) < 0) return nullptr;
   PyObject* m = PyModule_Create(&module);
   if (!m) return nullptr;
-  PyObject* names = PyTuple_New(sizeof(functions) / sizeof(functions[0]));
-  if (!names) return nullptr;
-  for (size_t i = 0; i < sizeof(functions) / sizeof(functions[0]); ++i)
-    PyTuple_SET_ITEM(names, i, PyUnicode_FromString(functions[i].name));
-  if (PyModule_AddObject(m, "FUNCTIONS", names) < 0) return nullptr;
+  constexpr int kAll = sizeof(functions) / sizeof(functions[0]);
+  const struct { const char* name; int first, end; } lists[] = {{"FUNCTIONS", 0, kDecoding}, {"QUANT_FUNCTIONS", kDecoding, kAll}};
+  for (const auto& list : lists) {
+    PyObject* names = PyTuple_New(list.end - list.first);
+    if (!names) return nullptr;
+    for (int i = list.first; i < list.end; ++i) PyTuple_SET_ITEM(names, i - list.first, PyUnicode_FromString(functions[i].name));
+    if (PyModule_AddObject(m, list.name, names) < 0) return nullptr;
+  }
   return m;
 }
