@@ -292,9 +292,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x002, 56 / kSteps, 0);
     }
-    // The logits' last product stays in front of the second product: left to the compiler it sinks behind that, to the branch in front
-    // of the next maxima.  There it waits in the matrix pipe for the product before it, for longer than the compiler's distance to its
-    // first reader allows for, and that reader (two logits of a lane) now and then saw the sum of seven eighths of the row.
+    // (the products stay here: left to the compiler the last one sinks to the branch in front of the next maxima, see settle())
     asm volatile("" : "+v"(next));
     __builtin_amdgcn_sched_barrier(0);
     s = next;
@@ -324,6 +322,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     read_k(ic<1 - u % 2>{});
     __builtin_amdgcn_sched_barrier(0);
     second_product();
+    __builtin_amdgcn_sched_barrier(0);       // in front of what follows, not as far behind it as its first reader allows: see settle()
     store_step(ic<(u + 1) % PF>{}, ic<(u + 1) % 2>{});
     load_step(ic<(u + 1) % PF>{}, t + 1 + PF);
     const int j = t * KG + kg;
@@ -347,6 +346,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     }
   }
   second_product();
+  settle(acc_o);
 
   run_sum = halves_sum(run_sum);
   const int64_t slot = static_cast<int64_t>(split) * p.Hq * p.T + g * M + row0 + c32;

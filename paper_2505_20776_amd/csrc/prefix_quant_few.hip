@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kWaves * 64) void prefix_quant_few_kernel(uint64_t 
       for (int i = 0; i < 2 * kPieces; ++i)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[rb][i], s[rb], 0, 0, 0);
-      // (the products stay here, far in front of the first reader of their results: see prefix_quant.hip)
+      // (the products stay here, far in front of the first reader of their results: see settle())
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(s[rb]));
       // V: widened while the logits come out of the matrix pipe
@@ -325,7 +325,10 @@ __global__ __launch_bounds__(kWaves * 64) void prefix_quant_few_kernel(uint64_t 
   // ---- the four waves' partials of a block of rows meet in LDS
   float* dump = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) run_sum[rb] = halves_sum(run_sum[rb]);
+  for (int rb = 0; rb < RB; ++rb) {
+    settle(acc_o[rb]);
+    run_sum[rb] = halves_sum(run_sum[rb]);
+  }
   __syncthreads();                                   // every wave is done with its ring
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) dump_wave<D>(dump, kWaves * RB, wave * RB + rb, acc_o[rb], ref[rb], run_sum[rb], lane);

@@ -240,3 +240,10 @@ def test_cache_beyond_32_bits():
     want = torch.exp(s - total) @ x
     assert abs(float(lse) - float(total)) <= 2.0 ** -16 * float(s.max())
     assert ((out.cpu().double() - want).abs() <= 2.0 ** -9 * want.abs().max()).all()
+
+
+@pytest.mark.parametrize("t", [8, 16, 30, 60])
+def test_sharp_rows_of_many_problems(t):
+    """The largest logit of every tile is seen by the running reference, whatever the order in which the products leave the matrix pipe."""
+    for seed in range(20, 28):
+        _Problem(seed, 128, 8, 2, t, 900, 32, sharp=16.0).check()
