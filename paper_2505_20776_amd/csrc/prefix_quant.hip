@@ -17,6 +17,14 @@
 // workgroup and stores them to one of two LDS buffers, while the waves compute on the other: one barrier per stage of KG tiles.
 // From there on the tile is that of the bf16 kernels: S^T = K Q^T and O^T += V^T P^T with a lane owning one query row in both
 // products, V through the transposing LDS read, P straight from the accumulator registers.
+//
+// Bound by no single unit: with 256 rows at 32K keys the matrix pipes are busy for 46 % of the time, the vector ALUs (widening,
+// exponentials, conversions, addresses) for 53 %, the LDS for 36 %, and under this load the package lowers its clock.  So the steps of
+// a tile are laid so that they overlap: behind the barrier the second product of the tile before, from registers, while K comes from
+// LDS (128 nodes of 32 heads in 8 groups at 32K keys 71 us per launch, 78 with it in front); then the next tile's logits while V
+// comes and the vector ALUs take the exponentials of this one (82 us per attention call, 91 with logits and softmax of one tile behind
+// each other).  Now, per launch: 128 nodes 32K 72 us, 0.95 PFLOP/s; 60 nodes 16K 25.5 (cache at 7.08 TB/s 4.8, products at the
+// 1.37 PFLOP/s of a large bf16 product 11.8), 2K 11.3; 30 nodes 16K 21; 60 nodes of 64-wide heads 8K 12.7.
 #include "quant_merge.h"
 
 namespace specext {
@@ -322,9 +330,16 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     read_k(ic<1 - u % 2>{});
     __builtin_amdgcn_sched_barrier(0);
     second_product();
-    __builtin_amdgcn_sched_barrier(0);       // in front of what follows, not as far behind it as its first reader allows: see settle()
     store_step(ic<(u + 1) % PF>{}, ic<(u + 1) % 2>{});
     load_step(ic<(u + 1) % PF>{}, t + 1 + PF);
+    // the products among the first of the conversions, not as late as their first reader allows (see settle()): 60 nodes at 16K keys
+    // 25.4 us per launch, 26.5 with all of them in front of the conversions
+#pragma unroll
+    for (int i = 0; i < 2 * kBlocks; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(0x002, 1, 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     const int j = t * KG + kg;
     if (__builtin_expect(wave_live && j < n_tiles, 1)) tile(j, ic<u % 2>{});
     else p0 = p1 = halfx8{};
