@@ -451,17 +451,18 @@ int specext_num_splits(const specext_desc* desc);
  * become +-448, NaN stays NaN.  A scale that grows moves the older rows of its block under the new one: exact for powers
  * of two but for magnitudes below 2^-15 of the largest, which round to steps of 2^-18 of it.  Rows behind the new
  * ones stay as they are and hold nothing until they are written (a write into a block takes the block's scale for that
- * of its older rows only).  The readers take any positive normal scale; a prefix for specext_verify_attn_quant needs
+ * of its older rows only).  The readers take any positive normal scale, and so does a write into a block that has one (x / scale
+ * is then x times the rounded reciprocal); a prefix for specext_verify_attn_quant needs
  * magnitudes of V within 2^-100 ... 2^100.
  *
  * head_dim 64 or 128; dtype is that of the caller's rows, SPECEXT_BF16 or SPECEXT_F32.  Strides are in elements
  * (cache_stride_*: bytes; scale_stride_*: floats), 0 = contiguous in the shapes given; rows of head_dim elements are
- * contiguous, strides in bytes multiples of 16, cache and row pointers 16-byte aligned.
+ * contiguous, strides in bytes multiples of 16, cache and row pointers 16-byte aligned; cache_capacity <= 2^28.
  */
 
 /*
  * n_tokens rows enter the cache at token `start`: k_src, v_src [n_layers, n_kv_heads, n_tokens, head_dim] of dtype.
- * start + n_tokens <= cache_capacity; n_tokens = 0 does nothing.
+ * start + n_tokens <= cache_capacity; n_tokens = 0 does nothing (k_src and v_src may be NULL then).
  */
 int specext_quant_kv_write(const void* k_src, const void* v_src, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
                            int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t n_tokens, int32_t start,
@@ -472,7 +473,7 @@ int specext_quant_kv_write(const void* k_src, const void* v_src, void* k_cache, 
 /*
  * Rows start ... start + n_tokens - 1 of the cache as bf16 or fp32 values, k_dst, v_dst [n_layers, n_kv_heads, n_tokens,
  * head_dim] of dtype: value = code x scale, rounded to dtype (exact in bf16 for scales that are powers of two).  For
- * specext_prefill_attn of a later piece of a prompt, and whatever else wants the cache's rows.
+ * specext_prefill_attn of a later piece of a prompt, and whatever else wants the cache's rows.  n_tokens = 0 does nothing.
  */
 int specext_quant_kv_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, void* k_dst, void* v_dst,
                           int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t n_tokens, int32_t start, int32_t cache_capacity,
@@ -482,8 +483,8 @@ int specext_quant_kv_read(const void* k_cache, const void* v_cache, const float*
 
 /*
  * specext_commit_tree_kv into an 8-bit cache: cache[y, g, prefix_len + i, :] = tree[y, g, path[i], :] for i < n_accept.
- * path holds min(max_accept, n_tree) entries; the count is clamped to that.  An entry that is no node leaves its
- * cache row as it is.  n_tree and max_accept <= 128, prefix_len + max_accept <= cache_capacity.
+ * path holds min(max_accept, n_tree) entries; the count is clamped to that.  An entry that is no node leaves the
+ * codes of its row as they are, and so does a count of 0 everything.  n_tree and max_accept <= 128, prefix_len + max_accept <= cache_capacity.
  */
 int specext_commit_tree_quant(const void* k_tree, const void* v_tree, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
                               const int32_t* path, const int32_t* n_accept, int32_t max_accept, int32_t n_tree, int32_t n_layers,
@@ -521,7 +522,8 @@ int specext_verify_attn_quant(const specext_desc* desc, const void* q, const voi
  *
  * Minus infinity bans a token.  A row of nothing else has lse and log probabilities of minus infinity, entropy 0 and the
  * lowest indices.  A row that holds NaN or plus infinity has NaN for lse, entropy and log probabilities; NaN ranks
- * highest.  vocab <= 2^20, n_rows <= 2^24; n_rows = 0 does nothing.  Results are bit-reproducible.
+ * highest.  vocab <= 2^20, n_rows x ceil((vocab + 5) / 16384) < 2^23, n_given <= 2^20, logit_scale 0 or within 2^-100 ...
+ * 2^100; n_rows = 0 does nothing (pointers but the workspace's may be NULL then).  Results are bit-reproducible.
  */
 size_t specext_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t k);
 int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride, float logit_scale,

@@ -15,6 +15,9 @@ inline bool aligned(const void* ptr, uintptr_t to) { return (reinterpret_cast<ui
 
 int block_log2_of(int32_t scale_block) { return scale_block == 32 ? 5 : scale_block == 64 ? 6 : scale_block == 128 ? 7 : -1; }
 
+// A launch has fewer than 2^32 threads along x: 256 for every 32 tokens written.
+constexpr int32_t kMaxCapacity = 1 << 28;
+
 // What the cache functions share: shape, cache and scale strides (bytes and floats), the caller's bf16 or fp32 rows.
 struct CacheShape {
   int64_t row_sy, row_sh, row_st, cache_sy, cache_sh, cache_sl, scale_sy, scale_sh;
@@ -24,14 +27,14 @@ int check_cache(const void* k_rows, const void* v_rows, const void* k_cache, con
                 int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t rows, int32_t n_tokens, int32_t start,
                 int32_t cache_capacity, int32_t scale_block, int64_t row_sy, int64_t row_sh, int64_t row_st, int64_t cache_sy,
                 int64_t cache_sh, int64_t cache_sl, int64_t scale_sy, int64_t scale_sh, CacheShape* c) {
-  if (!k_rows || !v_rows || !k_cache || !v_cache || !k_scale || !v_scale) return SPECEXT_ERR_INVALID_ARG;
+  if ((n_tokens != 0 && (!k_rows || !v_rows)) || !k_cache || !v_cache || !k_scale || !v_scale) return SPECEXT_ERR_INVALID_ARG;
   if (n_layers <= 0 || n_kv_heads <= 0 || head_dim <= 0 || n_tokens < 0 || start < 0 || rows < 0) return SPECEXT_ERR_INVALID_ARG;
   if (row_sy < 0 || row_sh < 0 || row_st < 0 || cache_sy < 0 || cache_sh < 0 || cache_sl < 0 || scale_sy < 0 || scale_sh < 0)
     return SPECEXT_ERR_INVALID_ARG;
   if (static_cast<int64_t>(start) + n_tokens > cache_capacity) return SPECEXT_ERR_INVALID_ARG;
   c->block_log2 = block_log2_of(scale_block);
   if (c->block_log2 < 0 || (head_dim != 64 && head_dim != 128) || (dtype != SPECEXT_F32 && dtype != SPECEXT_BF16) ||
-      cache_capacity > (1 << 30) || static_cast<int64_t>(n_layers) * n_kv_heads > 65535)
+      cache_capacity > kMaxCapacity || static_cast<int64_t>(n_layers) * n_kv_heads > 65535)
     return SPECEXT_ERR_UNSUPPORTED;
   const int64_t elem = dtype == SPECEXT_BF16 ? 2 : 4;
   const int64_t blocks = (static_cast<int64_t>(cache_capacity) + scale_block - 1) / scale_block;
@@ -140,8 +143,10 @@ int specext_quant_kv_read(const void* k_cache, const void* v_cache, const float*
 namespace {
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+// (a launch has fewer than 2^32 threads along x: 512 for a slice, which is 16384 fp32 values where rows are many)
 bool logprob_shape_ok(int32_t n_rows, int32_t vocab, int32_t k) {
-  return n_rows >= 0 && vocab > 0 && k >= 0 && k <= vocab && vocab <= kMaxVocab && k <= kMaxTop && n_rows <= (1 << 24);
+  return n_rows >= 0 && vocab > 0 && k >= 0 && k <= vocab && vocab <= kMaxVocab && k <= kMaxTop &&
+         static_cast<int64_t>(n_rows) * ((vocab + 4) / 16384 + 1) < (1 << 23);
 }
 size_t stats_bytes(int32_t n_rows, int slices) { return align_up(static_cast<size_t>(n_rows) * slices * 4 * sizeof(float)); }
 }  // namespace
@@ -163,16 +168,16 @@ int specext_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, in
                            float* lse, float* entropy, void* workspace, size_t workspace_bytes, void* stream) {
   if (n_rows < 0 || vocab <= 0 || n_given < 0 || k < 0 || k > vocab || row_stride < 0) return SPECEXT_ERR_INVALID_ARG;
   if (!(logit_scale >= 0.f) || std::isinf(logit_scale)) return SPECEXT_ERR_INVALID_ARG;
-  if (!logits || !workspace || (n_given > 0 && (!tokens || !logprob)) || (k > 0 && !top_id)) return SPECEXT_ERR_INVALID_ARG;
+  if (!workspace || (n_rows > 0 && (!logits || (n_given > 0 && (!tokens || !logprob)) || (k > 0 && !top_id)))) return SPECEXT_ERR_INVALID_ARG;
   const int64_t stride = row_stride ? row_stride : vocab;
   if (stride < vocab) return SPECEXT_ERR_INVALID_ARG;
+  if (logit_scale != 0.f && (logit_scale < 0x1p-100f || logit_scale > 0x1p100f)) return SPECEXT_ERR_UNSUPPORTED;
   if (!logprob_shape_ok(n_rows, vocab, k) || n_given > (1 << 20) || (dtype != SPECEXT_F32 && dtype != SPECEXT_BF16)) return SPECEXT_ERR_UNSUPPORTED;
   if (!aligned(logits, dtype == SPECEXT_BF16 ? 2 : 4) || !aligned(tokens, 4) || !aligned(logprob, 4) || !aligned(top_id, 4) ||
       !aligned(top_logprob, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(workspace, kAlign))
     return SPECEXT_ERR_UNSUPPORTED;
   if (workspace_bytes < specext_token_logprobs_bytes(n_rows, vocab, k)) return SPECEXT_ERR_WORKSPACE_TOO_SMALL;
   const LogprobCut cut = logprob_cut(n_rows, vocab, dtype == SPECEXT_BF16);
-  if (static_cast<int64_t>(n_rows) * cut.slices > (int64_t{1} << 30)) return SPECEXT_ERR_UNSUPPORTED;
   LogprobArgs a;
   std::memset(&a, 0, sizeof(a));
   a.logits = logits, a.tokens = tokens, a.logprob = logprob, a.top_id = top_id, a.top_logprob = top_logprob, a.lse = lse, a.entropy = entropy;

@@ -247,3 +247,19 @@ def test_sharp_rows_of_many_problems(t):
     """The largest logit of every tile is seen by the running reference, whatever the order in which the products leave the matrix pipe."""
     for seed in range(20, 28):
         _Problem(seed, 128, 8, 2, t, 900, 32, sharp=16.0).check()
+
+
+@pytest.mark.parametrize("d,t", [(128, 8), (128, 16), (128, 30), (128, 60), (64, 5)])
+def test_a_row_of_nan_stays_alone(d, t):
+    """A query of NaN (a padded row) answers with NaN and leaves the other rows as they are."""
+    p = _Problem(77, d, 8, 2, t, 300, 32)
+    p.q[t // 2, 3] = math.nan
+    out, lse, _ = p.run(0, True)
+    assert torch.isnan(out[t // 2, 3]).all() and torch.isnan(lse[3, t // 2])
+    want, want_lse, mag, spread, _ = p.reference()
+    rest = torch.ones((t, 8), dtype=torch.bool)
+    rest[t // 2, 3] = False
+    off_logit = 2.0 ** -16 * spread
+    tol = (2.0 ** -10 + (p.n + t) * 2.0 ** -24 + 2 * off_logit.T)[:, :, None] * mag[:, :, None]
+    assert ((out - want).abs() <= tol)[rest].all()
+    assert ((lse - want_lse).abs() <= off_logit + 2.0 ** -18 * (1 + want_lse.abs())).T[rest].all()

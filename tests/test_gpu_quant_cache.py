@@ -208,3 +208,21 @@ def test_nothing_to_do():
     sx.quant_kv_read(*c.codes, *c.scales, x, x, 1, 1, 64, 0, 3, 8, 32)
     torch.cuda.synchronize()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, c.codes + c.scales)) and (x == 1).all()
+
+
+def test_count_of_nothing_changes_nothing():
+    """In the middle of a block too, whatever its scale is."""
+    import paper_2505_20776_amd as sx
+    for scale in (2.0 ** -120, 0.3, 1.0):
+        c = _Pair(2, 2, 64, 64, 32)
+        for t in c.codes:
+            t.view(torch.uint8).copy_(torch.randint(0, 0x7F, t.shape, dtype=torch.uint8))
+        for t in c.scales:
+            t.fill_(scale)
+        before = [t.clone() for t in c.codes + c.scales]
+        x = torch.ones((2, 2, 8, 64), dtype=BF16, device="cuda")
+        for n in (0, -3):
+            sx.commit_tree_quant(x, x, *c.codes, *c.scales, torch.arange(8, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda"),
+                                 8, 8, 2, 2, 64, 37, 64, 32)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, c.codes + c.scales))

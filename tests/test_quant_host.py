@@ -157,3 +157,36 @@ def test_the_reported_split_count_holds_at_every_length(sx, d, hq, hkv, T):
             auto = sx.make_desc(**kw)
             asked = sx.make_desc(num_splits=sx.num_splits(auto), **kw)
             assert sx.num_splits(asked) == sx.num_splits(auto) and sx.workspace_bytes(asked) == sx.workspace_bytes(auto), (L, chunk)
+
+
+def test_nothing_to_do_needs_no_rows(sx):
+    """Empty tensors have no address."""
+    for f in (sx.quant_kv_write, sx.quant_kv_read):
+        a = [OK] * 6
+        for i in ((0, 1) if f is sx.quant_kv_write else (4, 5)):
+            a[i] = None
+        assert f(*a, **CACHE, n_tokens=0, start=1024) == 0
+        assert f(*a, **CACHE, n_tokens=1, start=0) == -1
+    assert sx.commit_tree_quant(None, None, *[OK] * 6, **CACHE, max_accept=0, n_tree=4, prefix_len=8) == 0
+    kw = dict(n_given=2, k=3, workspace_nbytes=sx.token_logprobs_bytes(0, 50, 3), stream=0, check=False)
+    assert sx.token_logprobs(None, 0, 50, OK, **kw) == 0
+    assert sx.token_logprobs(None, 0, 50, None, **kw) == -1
+    assert sx.token_logprobs(None, 1, 50, OK, **kw) == -1
+
+
+def test_sizes_beyond_one_launch(sx):
+    """Threads along x stay below 2^32."""
+    kw = dict(CACHE, n_layers=1, n_kv_heads=1, n_tokens=1 << 28, start=0)
+    for f in (sx.quant_kv_write, sx.quant_kv_read):
+        assert f(*[OK] * 6, **{**kw, "cache_capacity": (1 << 28) + 1}) == -2
+        assert f(*[OK] * 4, None, OK, **{**kw, "cache_capacity": 1 << 28}) == -1          # (the sizes themselves are allowed)
+    for rows, vocab, allowed in ((8388607, 10, True), (8388608, 10, False), (131071, 1 << 20, False), (129055, 1 << 20, True), (8388607, 16379, True),
+                                 (8388607, 16380, False), (4194303, 16380, True)):
+        assert (sx.token_logprobs_bytes(rows, vocab, 1) > 0) == allowed, (rows, vocab)
+        if not allowed:
+            assert sx.token_logprobs(OK, rows, vocab, OK, workspace_nbytes=1 << 50, stream=0, check=False) == -2
+
+
+@pytest.mark.parametrize("scale,status", [(2.0 ** -101, -2), (2.0 ** 101, -2), (1e-45, -2), (2.0 ** -100, -3), (2.0 ** 100, -3), (0.0, -3)])
+def test_range_of_the_logit_scale(sx, scale, status):
+    assert sx.token_logprobs(OK, 1, 50, OK, logit_scale=scale, workspace_nbytes=0, stream=0, check=False) == status
