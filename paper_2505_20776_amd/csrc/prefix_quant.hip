@@ -268,6 +268,7 @@ __global__ __launch_bounds__(R * KG * 64) void prefix_quant_kernel(uint64_t k_at
     for (int r = 2; r < 16; r += 2) top = fmaxf(top, fmaxf(s[r], s[r + 1]));
     top = fmaf(top, ct, lsv);                                    // the row's largest, the values' scale included
     if (__builtin_expect(__any(top > ref + kLazyLog2), 0)) {     // some row of this wave outgrew its reference: move every reference up
+      settle(acc_o);             // (rare, and the products of the tile before may be just behind)
       const float new_ref = fmaxf(ref, halves_max(top));
       const float alpha = fast_exp2(ref - new_ref);              // 0 on the first tile
       ref = new_ref;
