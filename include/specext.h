@@ -13,6 +13,9 @@
  *     (UpdateDraftCache).
  *   - The rest of the step in Alg. 1: greedy acceptance along the draft tree and
  *     the commit of the accepted tokens' K/V rows into the target cache.
+ *   - The same step over a target cache held in 8 bits, that cache's writing and
+ *     reading, and what a step reads from logits (most probable tokens, log
+ *     probabilities, entropy).
  *
  * Conventions common to every entry point
  *   - Every tensor argument is a DEVICE pointer owned by the caller.  The
@@ -449,7 +452,7 @@ int specext_num_splits(const specext_desc* desc);
  * largest finite magnitude of the block's new rows to at most 448, and not below 2^-100; where the block holds rows in
  * front of the new ones, at least the scale that it has.  Codes are x / scale to the nearest, ties to even; infinities
  * become +-448, NaN stays NaN.  A scale that grows moves the older rows of its block under the new one: exact for powers
- * of two but for magnitudes below 2^-15 of the largest, which round to steps of 2^-18 of it.  Rows behind the new
+ * of two but for magnitudes below 2^-6 of the scale, which round to steps of 2^-9 of it.  Rows behind the new
  * ones stay as they are and hold nothing until they are written (a write into a block takes the block's scale for that
  * of its older rows only).  The readers take any positive normal scale, and so does a write into a block that has one (x / scale
  * is then x times the rounded reciprocal); a prefix for specext_verify_attn_quant needs

@@ -5,7 +5,7 @@
 //   code     = e4m3(x / scale), to the nearest, ties to even;  x = code scale
 //
 // A power of two only moves the exponent of a code, so rows that are there already lose nothing when a later one needs a larger
-// scale (codes that leave the normal range, 2^-15 of the block's largest value, round to a step of 2^-18 of it).
+// scale (codes that leave the normal range, 2^-6 and more, round to steps of 2^-9).
 //
 // One workgroup has one block of one head, of K or of V: it holds the block's new rows in registers, finds their largest
 // magnitude, and writes codes and scale, so the rows are read once and no two workgroups share a scale.
