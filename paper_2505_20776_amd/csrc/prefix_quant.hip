@@ -24,7 +24,7 @@
 // LDS (128 nodes of 32 heads in 8 groups at 32K keys 71 us per launch, 78 with it in front); then the next tile's logits while V
 // comes and the vector ALUs take the exponentials of this one (82 us per attention call, 91 with logits and softmax of one tile behind
 // each other).  Now, per launch: 128 nodes 32K 72 us, 0.95 PFLOP/s; 60 nodes 16K 25.5 (cache at 7.08 TB/s 4.8, products at the
-// 1.37 PFLOP/s of a large bf16 product 11.8), 2K 11.3; 30 nodes 16K 21; 60 nodes of 64-wide heads 8K 12.7.
+// 1.37 PFLOP/s of a large bf16 product 11.8), 2K 11.3; 30 nodes 16K 19.4; 60 nodes of 64-wide heads 8K 12.7.
 #include "quant_merge.h"
 
 namespace specext {

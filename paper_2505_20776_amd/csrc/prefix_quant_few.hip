@@ -10,8 +10,9 @@
 // With one block of rows the load bounds it: 32 heads in 8 groups, one node, 131035 keys 46.3 us per launch, 5.8 TB/s (37.9 us at
 // the 7.08 of a plain read); 16K 11.1 (4.7), 2K 5.3 (0.6): what a launch, the first load and the end take.  With two blocks a wave
 // has 32 products per tile behind one another and a softmax for each block, and one wave per SIMD has nothing to put into the gaps:
-// 16 nodes 131035 keys 54 to 58, 2K 9.9; 12 heads of 64, one node, 1013 keys 4.8.  Per attention call one node at 2K takes 8.4 us,
-// 16 nodes at 131035 61; with the shared tiles and barriers of prefix_quant.hip they were 11.3 and 68.
+// 16 nodes 131035 keys 54 to 57; 2K 8.8, of which the end takes 2.8 and the tiles 1.8; 60 nodes of 12 64-wide heads at 1013 keys 5.6.
+// Per attention call one node at 2K takes 8.4 us, 16 nodes at 131035 60; with the shared tiles and barriers of prefix_quant.hip they
+// were 11.3 and 68.
 #include "quant_merge.h"
 
 namespace specext {

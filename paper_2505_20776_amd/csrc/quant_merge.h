@@ -17,27 +17,25 @@ __device__ __forceinline__ void settle(floatx16 (&acc)[N]) {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A wave's O^T accumulators in LDS, one register of all lanes behind the other; 65 words apart, so that lanes which read one row of
-// several registers hit different banks.
-constexpr int kDumpStride = 65;
+// A wave's O^T accumulators in LDS, four registers of a lane at a time: 16 bytes are four columns of a row.  The lanes' upper half lies
+// one such piece further, and so does every four registers twice, so that neighbouring lanes of a row, which read them in turns, and
+// the next rows beside them, hit different banks.  (Single words, with bank conflicts in their reads: 16 nodes of 32 heads in 8 groups at
+// 2K keys 9.85 us per prefix launch, now 8.8.)
+constexpr int kDumpHalf = 33, kDumpStride = 66;          // pieces
 template <int D>
-__host__ __device__ constexpr int dump_floats() { return D / 2 * kDumpStride; }
+__host__ __device__ constexpr int dump_floats() { return D / 8 * kDumpStride * 4; }
 // LDS of `waves` (waves x blocks of rows) dumps with their references and sums
 template <int D>
 __host__ __device__ constexpr int merge_bytes(int waves) { return waves * (dump_floats<D>() + 2 * 32) * 4; }
 
 template <int D>
 __device__ __forceinline__ void dump_wave(float* lds, int n_waves, int index, const floatx16 (&acc)[D / 32], float ref, float sum, int lane) {
-  float* at = lds + index * dump_floats<D>();
+  floatx4* at = reinterpret_cast<floatx4*>(lds + index * dump_floats<D>()) + (lane & 31) + (lane >> 5) * kDumpHalf;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) at[(db * 16 + r) * kDumpStride + lane] = acc[db][r];
-  float* ml = lds + n_waves * dump_floats<D>() + index * 64;
-  if (lane < 32) {
-    ml[lane] = ref;
-    ml[32 + lane] = sum;
-  }
+    for (int r = 0; r < 4; ++r) at[(db * 4 + r) * kDumpStride] = floatx4{acc[db][4 * r], acc[db][4 * r + 1], acc[db][4 * r + 2], acc[db][4 * r + 3]};
+  if (lane < 32) reinterpret_cast<floatx2*>(lds + n_waves * dump_floats<D>())[index * 32 + lane] = floatx2{ref, sum};
 }
 
 // Rows [0, n_rows) of a block, from dumps index0 + w * index_step of its GROUPS waves; this wave is number `member` of the GROUPS that
@@ -49,27 +47,27 @@ __device__ __forceinline__ void merge_groups(const float* lds, int n_waves, int 
                                              float* part_ml, int64_t slot0, int lane) {
   constexpr int kLanes = D / 4;                  // of a row: four columns each
   constexpr int kRows = 64 / kLanes;
-  const float* ml = lds + n_waves * dump_floats<D>();
+  const floatx2* ml = reinterpret_cast<const floatx2*>(lds + n_waves * dump_floats<D>());
   const int q = lane % kLanes;                   // columns 4 q .. 4 q + 3: registers 4 (q / 2) .. + 3 of lanes row + 32 (q & 1)
+  const int piece = (q >> 1) * kDumpStride + (q & 1) * kDumpHalf;
 #pragma unroll 4
   for (int row0 = member * kRows; row0 < min(n_rows, 32); row0 += GROUPS * kRows) {
     const int row = row0 + lane / kLanes;
-    float ref[GROUPS], sum[GROUPS];
+    floatx2 part[GROUPS];                        // reference, sum
     float top = -INFINITY, total = 0.f;
 #pragma unroll
     for (int w = 0; w < GROUPS; ++w) {
-      ref[w] = ml[(index0 + w * index_step) * 64 + row];
-      sum[w] = ml[(index0 + w * index_step) * 64 + 32 + row];
-      top = fmaxf(top, ref[w]);
+      part[w] = ml[(index0 + w * index_step) * 32 + row];
+      top = fmaxf(top, part[w][0]);
     }
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < GROUPS; ++w) {
-      const float weight = sum[w] > 0.f ? fast_exp2(ref[w] - top) : 0.f;       // a wave without tiles: nothing
-      total = fmaf(sum[w], weight, total);
-      const float* at = lds + (index0 + w * index_step) * dump_floats<D>() + (q >> 1) * 4 * kDumpStride + row + 32 * (q & 1);
+      const float weight = part[w][1] > 0.f ? fast_exp2(part[w][0] - top) : 0.f;       // a wave without tiles: nothing
+      total = fmaf(part[w][1], weight, total);
+      const floatx4 x = reinterpret_cast<const floatx4*>(lds + (index0 + w * index_step) * dump_floats<D>())[piece + row];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(at[e * kDumpStride], weight, o[e]);
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], weight, o[e]);
     }
     if constexpr (D == 128) {
       float largest = row16_max(fmaxf(fmaxf(fabsf(o[0]), fabsf(o[1])), fmaxf(fabsf(o[2]), fabsf(o[3]))));
