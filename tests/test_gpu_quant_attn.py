@@ -263,3 +263,24 @@ def test_a_row_of_nan_stays_alone(d, t):
     tol = (2.0 ** -10 + (p.n + t) * 2.0 ** -24 + 2 * off_logit.T)[:, :, None] * mag[:, :, None]
     assert ((out - want).abs() <= tol)[rest].all()
     assert ((lse - want_lse).abs() <= off_logit + 2.0 ** -18 * (1 + want_lse.abs())).T[rest].all()
+
+
+@pytest.mark.parametrize("t", [8, 16, 60])
+def test_two_calls_at_once(t):
+    """On two streams, each with a workspace of its own: the bits of the calls one after the other."""
+    made = []
+    for seed in (91, 92):
+        p = _Problem(seed, 128, 8, 2, t, 3000 + seed, 64)
+        p.run(32)
+        made.append((p, p.out.clone(), p.lse.clone(), torch.cuda.Stream()))
+    for p, _, _, _ in made:
+        p.out.zero_()
+        p.lse.zero_()
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for p, _, _, s in made:
+            with torch.cuda.stream(s):
+                p.call()
+    torch.cuda.synchronize()
+    for p, out, lse, _ in made:
+        assert torch.equal(p.out, out) and torch.equal(p.lse, lse)
